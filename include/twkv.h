@@ -79,6 +79,7 @@ typedef enum {
 #define TWKV_PIECE_TOKENS 131072    /* a compress call is processed in pieces of this many tokens    */
 #define TWKV_MAX_CLASSES 16
 #define TWKV_PREFILL_MAX_QUERIES 16384   /* queries per twkv_prefill_attn call                          */
+#define TWKV_TREE_MAX_NODES 64           /* nodes of one drafted tree                                   */
 
 typedef struct {
   int32_t n_layers;
@@ -205,6 +206,70 @@ twkv_status twkv_prefill_attn(twkv_cache* cache, int layer, const void* q, const
  * survivors.  Decode and prefill attention afterwards see the survivors only.
  */
 twkv_status twkv_evict(twkv_cache* cache, int layer, int seq, const int32_t* keep_positions, int n_keep, void* stream);
+
+/*
+ * Speculative decoding over the compressed cache (the paper has no counterpart; the states are treated as Eq. 1 to 8 say).
+ * A step drafts a tree of tokens behind each sequence, has the model look at all of them at once, and keeps one path:
+ *   twkv_slot_map     request lengths -> first row of every request, sequence id and position of every row
+ *   twkv_tree_map     parents -> position and ancestor mask of every node
+ *   twkv_tree_attn    per layer: attention of the nodes over their sequence's cached tokens and their ancestors
+ *   twkv_tree_accept  drafted and chosen tokens -> the rows of the path that is kept
+ * and twkv_compress stores the kept rows (their sequence ids and positions by twkv_slot_map of the numbers of kept nodes).
+ *
+ * Rows: request i has rows offsets[i] .. offsets[i + 1] - 1, its nodes in order; node 0 is the tree's root, usually the token
+ * sampled last, and every parent comes before its children.  All arrays are device memory and are read when the call runs, so
+ * that a captured step follows them; what the host has to know are upper bounds.  n_req is at most max_seqs.
+ */
+/*
+ * Rows of new tokens, for prompts, single tokens and trees alike, in the form that twkv_compress takes.
+ *   req_seqs  [n_req] int32 sequence ids; req_lens [n_req] int32 new rows of each (0 is fine)
+ *   starts    [n_req] int32 position of each request's first row, or NULL: the tokens now cached for the sequence in `layer` (a sequence
+ *             may then be listed once)
+ *   offsets   [n_req + 1] OUTPUT; seq_ids, positions [max_rows] OUTPUT: rows behind the last request's are left as they are
+ * Nothing but zero offsets is written, and the sticky status is set, where an id, length or position is out of range
+ * (TWKV_ERR_INVALID_ARG) or the rows are more than max_rows (TWKV_ERR_CAPACITY).
+ */
+twkv_status twkv_slot_map(twkv_cache* cache, int layer, const int32_t* req_seqs, const int32_t* req_lens, const int32_t* starts, int n_req,
+                          int max_rows, int32_t* offsets, int32_t* seq_ids, int32_t* positions, void* stream);
+/*
+ * Positions and ancestor masks of drafted trees.
+ *   offsets    [n_req + 1] as twkv_slot_map writes them; trees of at most max_nodes <= TWKV_TREE_MAX_NODES nodes, n_rows rows in all
+ *   parents    [n_rows] int32: number of the parent inside the tree, -1 for a root (node 0 is one)
+ *   positions  [n_rows] INPUT of every tree's first row, OUTPUT of the others: first + depth
+ *   masks      [n_rows] uint64 OUTPUT: bit k = node k of the tree is the row's node or an ancestor of it
+ * A tree with a parent that is not an earlier node of it gets zero masks and the sticky status TWKV_ERR_INVALID_ARG; the rows of one
+ * whose offsets are out of range are left alone.
+ */
+twkv_status twkv_tree_map(twkv_cache* cache, const int32_t* offsets, const int32_t* parents, int n_req, int n_rows, int max_nodes,
+                          int32_t* positions, uint64_t* masks, void* stream);
+/*
+ * Attention of drafted trees.  Node j of request i attends to every token cached for req_seqs[i] in `layer` and to the nodes of its own tree
+ * whose bits are set in masks[j] (any set of nodes; no node and no cached token: zeros).  The nodes are not in the cache: their states are
+ * given, with the ranks they would be stored with, and count as the cache would hold them.
+ *   q, out     [n_rows x n_q_heads x 128] dtype / out_dtype; q already rotated at its own position
+ *   K, V       [n_rows x d_kv] spectral states x~ of the nodes (pre-RoPE), dtype, row-major
+ *   levels     [n_rows x 2] uint16 (r_K, r_V), 1 <= r <= d_kv (e.g. of twkv_gate_ranks_static)
+ *   req_seqs   [n_req] int32, distinct; offsets, positions, masks as above
+ *   workspace  device memory, 256-byte aligned, of twkv_tree_required_bytes(cache, n_req, max_nodes) bytes.  Less, down to the bytes
+ *              for one request, is taken as well: the requests then run in several passes.  It holds nothing between calls, and calls that
+ *              overlap on the GPU must not share it (nor the cache's scratch).
+ * A request with an id, offset, rank or position out of range, or whose sequence or rows an earlier one names, gets zeros (where its rows
+ * are its own) and the sticky status is set.  A node whose V state is not finite makes the outputs of the nodes that see it NaN, no others.
+ */
+size_t twkv_tree_required_bytes(const twkv_cache* cache, int n_req, int max_nodes);
+twkv_status twkv_tree_attn(twkv_cache* cache, int layer, const void* q, const void* K, const void* V, const uint16_t* levels,
+                           const int32_t* req_seqs, const int32_t* offsets, const int32_t* positions, const uint64_t* masks, int n_req,
+                           int n_rows, int max_nodes, void* out, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * The path of every tree that verification keeps: node 0, then, as long as there is one, the lowest-numbered child of the current
+ * node whose drafted token is the token chosen behind it.
+ *   draft, target  [n_rows] int32: the node's own token, and the token that the model chooses behind it
+ *   n_accepted     [n_req] OUTPUT: nodes kept (0 for a tree without nodes)
+ *   rows           [n_rows] OUTPUT: the kept rows, request after request, in path order; entries behind the last are left as they are
+ *   next_tokens    [n_req] OUTPUT: the token chosen behind the last kept node, -1 for a tree without nodes
+ */
+twkv_status twkv_tree_accept(twkv_cache* cache, const int32_t* offsets, const int32_t* parents, const int32_t* draft, const int32_t* target,
+                             int n_req, int n_rows, int max_nodes, int32_t* n_accepted, int32_t* rows, int32_t* next_tokens, void* stream);
 
 /* Synchronises `stream`, returns the sticky device status and clears it. */
 twkv_status twkv_cache_status(twkv_cache* cache, void* stream);

@@ -20,13 +20,14 @@ TWKV_F16, TWKV_BF16, TWKV_F32 = 0, 1, 2
 TWKV_GATE_FORCED, TWKV_GATE_LOGITS, TWKV_GATE_COMPUTE = 0, 1, 2
 TILE_TOKENS, PANEL_ELEMS, BLOCK_BYTES, PIECE_TOKENS, MAX_CLASSES = 128, 64, 16384, 131072, 16
 PREFILL_MAX_QUERIES = 16384
+TREE_MAX_NODES = 64
 
 EXPORTS = ["twkv_cache_required_bytes", "twkv_cache_create", "twkv_cache_destroy", "twkv_cache_reset",
            "twkv_cache_set_layer_params", "twkv_compress", "twkv_decode_attn", "twkv_prefill_attn", "twkv_evict", "twkv_cache_check", "twkv_selftest_wait_timeout", "twkv_cache_status",
            "twkv_cache_stats", "twkv_cache_layout", "twkv_launch_count", "twkv_status_string",
            "twkv_profile_enable", "twkv_profile_read", "twkv_gate_ranks_static", "twkv_gate_soft",
            "twkv_projector_required_bytes", "twkv_projector_create", "twkv_projector_destroy", "twkv_project",
-           "twkv_projector_status"]
+           "twkv_projector_status", "twkv_slot_map", "twkv_tree_map", "twkv_tree_required_bytes", "twkv_tree_attn", "twkv_tree_accept"]
 STATIC_GATE_MAX_ROWS = 1024
 KERNEL_KINDS = ["gate_gemm", "gate_rank", "hist", "alloc", "pack", "plan", "kscore", "vacc", "merge", "other"]
 
@@ -97,6 +98,16 @@ def _load():
     L.twkv_project.restype = i32
     L.twkv_projector_status.argtypes = [vp, vp]
     L.twkv_projector_status.restype = i32
+    L.twkv_slot_map.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+    L.twkv_slot_map.restype = i32
+    L.twkv_tree_map.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp]
+    L.twkv_tree_map.restype = i32
+    L.twkv_tree_required_bytes.argtypes = [vp, i32, i32]
+    L.twkv_tree_required_bytes.restype = sz
+    L.twkv_tree_attn.argtypes = [vp, i32] + [vp] * 8 + [i32] * 3 + [vp, vp, sz, vp]
+    L.twkv_tree_attn.restype = i32
+    L.twkv_tree_accept.argtypes = [vp] * 5 + [i32] * 3 + [vp] * 4
+    L.twkv_tree_accept.restype = i32
     L.twkv_launch_count.argtypes = []
     L.twkv_launch_count.restype = ctypes.c_uint64
     L.twkv_status_string.argtypes = [i32]
@@ -235,6 +246,45 @@ def twkv_gate_soft(cache, layer, K, V, m_k=None, m_v=None, xh_k=None, xh_v=None,
     n = K.shape[0] if n_tok is None else n_tok
     _check(lib.twkv_gate_soft(cache, layer, _ptr(K), _ptr(V), n, _ptr(m_k), _ptr(m_v), _ptr(xh_k), _ptr(xh_v), _ptr(retain),
                               _stream(stream)), "twkv_gate_soft")
+
+
+def twkv_slot_map(cache, layer, req_seqs, req_lens, offsets, seq_ids, positions, starts=None, stream=None):
+    """Request lengths -> offsets [n_req + 1], seq_ids and positions of every new row (int32 CUDA tensors; the two last have room for
+    the rows the caller expects at most).  starts=None: every request starts behind the tokens cached for its sequence in `layer`."""
+    assert req_lens.numel() == req_seqs.numel() and offsets.numel() == req_seqs.numel() + 1 and seq_ids.numel() == positions.numel()
+    _check(lib.twkv_slot_map(cache, layer, _ptr(req_seqs), _ptr(req_lens), _ptr(starts), req_seqs.numel(), seq_ids.numel(), _ptr(offsets),
+                             _ptr(seq_ids), _ptr(positions), _stream(stream)), "twkv_slot_map")
+
+
+def twkv_tree_map(cache, offsets, parents, positions, masks, max_nodes=TREE_MAX_NODES, stream=None):
+    """Parents -> positions (int32, in place: every tree's first row is given) and ancestor masks (int64 CUDA tensor, one bit per node)."""
+    assert positions.numel() == parents.numel() and masks.numel() == parents.numel() and masks.element_size() == 8
+    _check(lib.twkv_tree_map(cache, _ptr(offsets), _ptr(parents), offsets.numel() - 1, parents.numel(), max_nodes, _ptr(positions), _ptr(masks),
+                             _stream(stream)), "twkv_tree_map")
+
+
+def twkv_tree_required_bytes(cache, n_req: int, max_nodes: int) -> int:
+    return int(lib.twkv_tree_required_bytes(cache, n_req, max_nodes))
+
+
+def twkv_tree_attn(cache, layer, q, K, V, levels, req_seqs, offsets, positions, masks, out, workspace, max_nodes=TREE_MAX_NODES, stream=None):
+    """Attention of drafted trees over the cached tokens of their sequences and their own ancestors.  q / out: [n_rows, Hq, 128];
+    K / V: [n_rows, d_kv] spectral states of the nodes, levels: [n_rows, 2] their ranks; workspace: 1-D uint8 CUDA tensor of
+    twkv_tree_required_bytes(cache, n_req, max_nodes) bytes (fewer: several passes)."""
+    n = q.shape[0]
+    assert K.shape[0] == n and V.shape[0] == n and levels.numel() == 2 * n and positions.numel() == n and masks.numel() == n and out.shape[0] == n
+    assert offsets.numel() == req_seqs.numel() + 1 and masks.element_size() == 8 and levels.element_size() == 2
+    _check(lib.twkv_tree_attn(cache, layer, _ptr(q), _ptr(K), _ptr(V), _ptr(levels), _ptr(req_seqs), _ptr(offsets), _ptr(positions), _ptr(masks),
+                              req_seqs.numel(), n, max_nodes, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                              _stream(stream)), "twkv_tree_attn")
+
+
+def twkv_tree_accept(cache, offsets, parents, draft, target, n_accepted, rows, next_tokens, max_nodes=TREE_MAX_NODES, stream=None):
+    """Drafted and chosen tokens -> kept nodes per request, their rows one request behind the other, and every request's next token."""
+    n, n_req = parents.numel(), offsets.numel() - 1
+    assert draft.numel() == n and target.numel() == n and rows.numel() == n and n_accepted.numel() == n_req and next_tokens.numel() == n_req
+    _check(lib.twkv_tree_accept(cache, _ptr(offsets), _ptr(parents), _ptr(draft), _ptr(target), n_req, n, max_nodes, _ptr(n_accepted), _ptr(rows),
+                                _ptr(next_tokens), _stream(stream)), "twkv_tree_accept")
 
 
 def twkv_cache_status(cache, stream=None) -> int:

@@ -7,7 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libtwkv.so")
-SOURCES = ["api.cu", "compress.cu", "gate_gemm.cu", "decode.cu", "kscore_tc.cu", "vacc_tc.cu", "prefill_tc.cu", "gate_tc.cu", "gate_logits_tc.cu", "gate_static.cu", "gate_soft.cu", "evict.cu", "selfcheck.cu", "project_tc.cu", "project_api.cu"]
+SOURCES = ["api.cu", "compress.cu", "gate_gemm.cu", "decode.cu", "kscore_tc.cu", "vacc_tc.cu", "prefill_tc.cu", "gate_tc.cu", "gate_logits_tc.cu", "gate_static.cu", "gate_soft.cu", "evict.cu", "tree_maps.cu", "tree_plan.cu", "tree_attn.cu", "selfcheck.cu", "project_tc.cu", "project_api.cu"]
 
 
 def _stale() -> bool:
@@ -22,7 +22,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
+    cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
            "-Xcompiler", "-fPIC", "-shared", "-I", INCLUDE, "-I", CSRC, "-o", LIB]
     if verbose:
         cmd += ["-Xptxas", "-v"]

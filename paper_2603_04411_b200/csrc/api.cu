@@ -12,6 +12,7 @@
 #include "twkv_dev.h"
 #include "tc_util.cuh"
 #include "prefill.h"
+#include "tree.h"
 
 namespace twkv {
 
@@ -822,6 +823,131 @@ twkv_status twkv_prefill_attn(twkv_cache* c, int layer, const void* q, const int
     const int off = wave_start[w], n = wave_start[w + 1] - off;
     twkv_status s = decode_pass(c, layer, q, w0 + off, n, out, num_splits, w0 + n_q + off, w0 + 2 * (size_t)n_q + off, st);
     if (s != TWKV_OK) return s;
+  }
+  return TWKV_OK;
+}
+
+// ------------------------------------------------------------------------------ drafted trees
+// Lays a pass of n_req requests out in the workspace (base null: sizes only) and returns its bytes.
+static size_t tree_layout(const twkv_cache* c, TreeCall& a, unsigned char* base) {
+  const DevView& v = c->view;
+  size_t at = 0;
+  auto take = [&](size_t bytes) -> unsigned char* {
+    unsigned char* p = base + at;
+    at += (bytes + 1023) / 1024 * 1024;
+    return p;
+  };
+  // (room for n_splits of a request each; counted so that more requests never ask for less)
+  const size_t n = a.n_req, tiles = (size_t)v.TPS + 1, fill = std::min(n * TREE_MAX_SPLITS, (size_t)c->sm_count / ((a.C + 63) / 64));
+  const size_t parts = std::max(n, fill) * a.T * v.Hq;
+  a.nk = take(n * v.NC * TREE_PANEL_ROWS * PANEL * 2);
+  a.nv = take(n * v.NC * TREE_PANEL_ROWS * PANEL * 2);
+  a.qop = (unsigned short*)take(n * v.Hkv * a.Rp * HEAD_DIM * 2);
+  a.seqmax = (unsigned*)take(n * a.C * sizeof(unsigned));
+  a.info = (int4*)take(n * sizeof(int4));
+  a.bad = (unsigned long long*)take(n * sizeof(unsigned long long));
+  a.klist = (int4*)take(n * a.entries * sizeof(int4));
+  a.vmeta = (int4*)take(n * tiles * sizeof(int4));
+  a.vcut = (int*)take(n * (a.n_splits + 1) * sizeof(int));
+  a.cta_start = (int*)take((MAX_PLAN_CTAS + 1) * sizeof(int));
+  a.parts = (int*)take(sizeof(int));
+  a.part_l = (float*)take(parts * sizeof(float));
+  a.part_acc = (float*)take(parts * v.d_kv * sizeof(float));
+  a.scores = (float*)take(n * tiles * TILE * a.C * sizeof(float));
+  return at;
+}
+
+// Shapes of a pass of n_req requests.
+static TreeCall tree_shape(const twkv_cache* c, int n_req, int max_nodes) {
+  const DevView& v = c->view;
+  TreeCall a = {};
+  a.n_req = n_req; a.T = max_nodes;
+  a.R = max_nodes * v.rep; a.Rs = (a.R + 3) & ~3; a.Rp = (a.R + 15) & ~15; a.C = v.Hkv * a.Rs;
+  a.entries = (v.TPS + 4) & ~1;
+  a.n_splits = std::max(1, std::min(TREE_MAX_SPLITS, c->sm_count / (n_req * ((a.C + 63) / 64))));
+  return a;
+}
+
+static bool tree_sizes_ok(const twkv_cache* c, int n_req, int max_nodes) {
+  return n_req >= 0 && n_req <= c->cfg.max_seqs && max_nodes >= 1 && max_nodes <= TWKV_TREE_MAX_NODES;
+}
+
+size_t twkv_tree_required_bytes(const twkv_cache* c, int n_req, int max_nodes) {
+  if (!c || !tree_sizes_ok(c, n_req, max_nodes) || n_req == 0) return 0;
+  TreeCall a = tree_shape(c, n_req, max_nodes);
+  return tree_layout(c, a, nullptr);
+}
+
+twkv_status twkv_slot_map(twkv_cache* c, int layer, const int32_t* req_seqs, const int32_t* req_lens, const int32_t* starts, int n_req, int max_rows,
+                          int32_t* offsets, int32_t* seq_ids, int32_t* positions, void* stream) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers || n_req < 0 || n_req > c->cfg.max_seqs || max_rows < 0) return TWKV_ERR_INVALID_ARG;
+  if (!offsets || (n_req > 0 && (!req_seqs || !req_lens)) || (max_rows > 0 && (!seq_ids || !positions))) return TWKV_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return TWKV_ERR_CUDA;
+  ProfBind pb(&c->prof);
+  if (launch_slot_map(c->view, layer, req_seqs, req_lens, starts, n_req, max_rows, offsets, seq_ids, positions, c->sm_count,
+                      (cudaStream_t)stream) != cudaSuccess) return TWKV_ERR_CUDA;
+  return TWKV_OK;
+}
+
+twkv_status twkv_tree_map(twkv_cache* c, const int32_t* offsets, const int32_t* parents, int n_req, int n_rows, int max_nodes, int32_t* positions,
+                          uint64_t* masks, void* stream) {
+  if (!c || !tree_sizes_ok(c, n_req, max_nodes) || n_rows < 0) return TWKV_ERR_INVALID_ARG;
+  if (n_req == 0 || n_rows == 0) return TWKV_OK;
+  if (!offsets || !parents || !positions || !masks || (uintptr_t)masks % 8) return TWKV_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return TWKV_ERR_CUDA;
+  ProfBind pb(&c->prof);
+  if (launch_tree_map(c->view, offsets, parents, n_req, n_rows, max_nodes, positions, (unsigned long long*)masks, (cudaStream_t)stream) != cudaSuccess)
+    return TWKV_ERR_CUDA;
+  return TWKV_OK;
+}
+
+twkv_status twkv_tree_accept(twkv_cache* c, const int32_t* offsets, const int32_t* parents, const int32_t* draft, const int32_t* target, int n_req,
+                             int n_rows, int max_nodes, int32_t* n_accepted, int32_t* rows, int32_t* next_tokens, void* stream) {
+  if (!c || !tree_sizes_ok(c, n_req, max_nodes) || n_rows < 0) return TWKV_ERR_INVALID_ARG;
+  if (n_req == 0) return TWKV_OK;
+  if (!offsets || !n_accepted || !next_tokens || (n_rows > 0 && (!parents || !draft || !target || !rows))) return TWKV_ERR_INVALID_ARG;
+  DeviceGuard g(c->device);
+  if (!g.ok) return TWKV_ERR_CUDA;
+  ProfBind pb(&c->prof);
+  if (launch_tree_accept(c->view, offsets, parents, draft, target, n_req, n_rows, max_nodes, n_accepted, rows, next_tokens,
+                         (cudaStream_t)stream) != cudaSuccess) return TWKV_ERR_CUDA;
+  return TWKV_OK;
+}
+
+twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* K, const void* V, const uint16_t* levels, const int32_t* req_seqs,
+                           const int32_t* offsets, const int32_t* positions, const uint64_t* masks, int n_req, int n_rows, int max_nodes, void* out,
+                           void* workspace, size_t workspace_bytes, void* stream) {
+  if (!c || layer < 0 || layer >= c->cfg.n_layers || !tree_sizes_ok(c, n_req, max_nodes) || n_rows < 0) return TWKV_ERR_INVALID_ARG;
+  if (n_req == 0 || n_rows == 0) return TWKV_OK;
+  if (!q || !K || !V || !levels || !req_seqs || !offsets || !positions || !masks || !out || !workspace) return TWKV_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)out) % 16 || (uintptr_t)levels % 4 || (uintptr_t)masks % 8 || (uintptr_t)workspace % 256)
+    return TWKV_ERR_INVALID_ARG;
+  if (!c->params[layer].Uinv_k || !c->params[layer].Uinv_v) return TWKV_ERR_INVALID_ARG;
+  // as many requests to a pass as the workspace holds
+  int group = n_req;
+  while (group > 0) {
+    TreeCall a = tree_shape(c, group, max_nodes);
+    if (tree_layout(c, a, nullptr) <= workspace_bytes) break;
+    group = group > 1 ? (group + 1) / 2 : 0;
+  }
+  if (group == 0) return TWKV_ERR_CAPACITY;
+  DeviceGuard g(c->device);
+  if (!g.ok) return TWKV_ERR_CUDA;
+  ProfBind pb(&c->prof);
+  cudaStream_t st = (cudaStream_t)stream;
+  const int n_pieces = c->sm_count / 2;
+  for (int r0 = 0; r0 < n_req; r0 += group) {
+    TreeCall a = tree_shape(c, std::min(group, n_req - r0), max_nodes);
+    tree_layout(c, a, (unsigned char*)workspace);
+    a.q = (const unsigned short*)q; a.K = (const unsigned short*)K; a.V = (const unsigned short*)V; a.levels = levels;
+    a.req_seqs = req_seqs; a.offsets = offsets; a.positions = positions; a.masks = (const unsigned long long*)masks;
+    a.out = out; a.n_rows = n_rows; a.r0 = r0;
+    if (launch_tree_plan(c->view, a, layer, n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
+    if (launch_tree_score(c->view, a, layer, c->params[layer], n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
+    if (launch_tree_value(c->view, a, st) != cudaSuccess) return TWKV_ERR_CUDA;
+    if (launch_tree_merge(c->view, a, c->params[layer], st) != cudaSuccess) return TWKV_ERR_CUDA;
   }
   return TWKV_OK;
 }

@@ -1,0 +1,69 @@
+// Attention of drafted trees over the cache (tree_*.cu): one call's arguments, its tables and its buffers in the caller's workspace.
+//
+// A request is a sequence and the nodes of its tree.  The nodes' own states lie in two tiles of the workspace, one of keys and one
+// of values, beside the sequence's tiles in the cache; a score row is a token's (or node's) scores with all query rows of the request:
+//   column (g Rs + t rep + h): KV head g, node t, query head h of the group; Rs = max_nodes rep rounded up to four
+// and rows lie in the order of the request's V tiles (in the order of the sequence's list, the nodes' tile behind them), 128 a tile.
+#pragma once
+#include <cuda.h>
+#include "twkv_dev.h"
+
+namespace twkv {
+
+constexpr int TREE_MAX_SPLITS = 64;              // of a request's V tiles
+constexpr int TREE_PANEL_ROWS = 64;              // rows of a panel of the nodes' tiles
+static_assert(TWKV_TREE_MAX_NODES <= TREE_PANEL_ROWS && TWKV_TREE_MAX_NODES <= 64, "a node is a bit of a 64-bit word, and a row of a panel");
+// K list entry: .x tile in the cache / ~ number of a joint tile / score tile of the nodes, .y class | flags | tokens << 16, .z first block
+// (nodes: first row of the panels), .w request
+constexpr int TREE_NODES = 0x4000, TREE_FILLER = 0x8000, TREE_CLASS = 0x1f;
+
+struct TreeCall {
+  // the caller's
+  const unsigned short *q, *K, *V, *levels;
+  const int *req_seqs, *offsets, *positions;
+  const unsigned long long* masks;
+  void* out;
+  int n_rows;           // rows of q, K, V, levels, positions, masks, out
+  // this pass: requests r0 .. r0 + n_req - 1 of the call
+  int r0, n_req;
+  int T;                // most nodes of a request
+  int R, Rs, Rp;        // query rows of a KV head: T rep; rounded up to 4 (score columns), to 16 (operand rows)
+  int C;                // columns of a score row, Hkv Rs
+  int n_splits;
+  int entries;          // room of a request in the K list
+  // workspace
+  unsigned short* qop;  // [n_req][Hkv][Rp][128] f16 queries in the order of the score contraction
+  unsigned char *nk, *nv;     // [n_req][NC][64 rows][64] panels of the nodes' keys and values
+  unsigned* seqmax;     // [n_req][C]
+  float* scores;        // [n_req][TPS + 1][128][C]
+  int4* info;           // [n_req] first row, nodes, sequence (-1: refused), V tiles of the sequence
+  unsigned long long* bad;    // [n_req] nodes whose values are not finite
+  int4* klist;          // entries of all requests, a request's from an even place on
+  int4* vmeta;          // [n_req][TPS + 1] V tiles in stride order: score tile, class, tokens, first block (-1: the nodes)
+  int* vcut;            // [n_req][n_splits + 1]
+  int *cta_start, *parts;     // [pieces + 1] first item part of a piece; parts of an item
+  float* part_acc;      // [n_req][T][n_splits][Hq][d_kv]
+  float* part_l;        // [n_req][T][n_splits][Hq]
+};
+
+// Rows of tree i; false where the offsets do not describe at most max_nodes rows of n_rows.
+__device__ __forceinline__ bool tree_rows(const int* offsets, int i, int n_rows, int max_nodes, int* first, int* n) {
+  const int a = offsets[i], b = offsets[i + 1];
+  const bool ok = a >= 0 && a <= b && b <= n_rows && b - a <= max_nodes;
+  *first = ok ? a : 0;
+  *n = ok ? b - a : 0;
+  return ok;
+}
+
+cudaError_t launch_slot_map(const DevView& v, int layer, const int* req_seqs, const int* req_lens, const int* starts, int n_req, int max_rows,
+                            int* offsets, int* seq_ids, int* positions, int sm_count, cudaStream_t st);
+cudaError_t launch_tree_map(const DevView& v, const int* offsets, const int* parents, int n_req, int n_rows, int max_nodes, int* positions,
+                            unsigned long long* masks, cudaStream_t st);
+cudaError_t launch_tree_accept(const DevView& v, const int* offsets, const int* parents, const int* draft, const int* target, int n_req, int n_rows,
+                               int max_nodes, int* n_accepted, int* rows, int* next_tokens, cudaStream_t st);
+cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int n_pieces, cudaStream_t st);
+cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, int layer, const LayerParams& lp, int n_pieces, cudaStream_t st);
+cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, cudaStream_t st);
+cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const LayerParams& lp, cudaStream_t st);
+
+}  // namespace twkv
