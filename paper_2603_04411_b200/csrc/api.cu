@@ -557,6 +557,19 @@ twkv_status twkv_compress(twkv_cache* c, int layer, const void* K, const void* V
   return TWKV_OK;
 }
 
+// The copy of U_K^-1 that the score kernels read.  First call after the parameters were (re)set: re-tiled into the contiguous K-major panels
+// the tensor cores read.
+static bool prepare_uinv(twkv_cache* c, int layer, cudaStream_t st) {
+  if (c->prepared[layer]) return true;
+  unsigned char* dst = c->pool + c->off.prep_uinvT + (size_t)layer * c->dims.d_kv * c->dims.d_kv * 2;
+  if (launch_uinv_panels(c->params[layer].Uinv_k, dst, c->dims.d_kv, st) != cudaSuccess) return false;
+  // box = a whole panel for the single-CTA kernel, the CTA's half of its rows for the pair kernel
+  if (!make_tmap_2d(&c->map_uinvT[layer], dst, (uint64_t)c->dims.NC * c->dims.d_kv, PANEL, PANEL * 2,
+                    c->kscore_pairs ? HEAD_DIM / 2 : HEAD_DIM)) return false;
+  c->prepared[layer] = !is_capturing(st);                // (as for the gate weights)
+  return true;
+}
+
 // One pass of the decode kernels: one query per listed sequence.  qmap / qpos (device, per query slot) are set for a
 // prefill wave: the row of q / out a slot stands for, and the last position it may attend to.
 static twkv_status decode_pass(twkv_cache* c, int layer, const void* q, const int32_t* seq_ids, int n_seq, void* out,
@@ -578,15 +591,7 @@ static twkv_status decode_pass(twkv_cache* c, int layer, const void* q, const in
   DeviceGuard g(c->device);
   if (!g.ok) return TWKV_ERR_CUDA;
   ProfBind pb(&c->prof);
-  if (!c->prepared[layer]) {
-    // first decode after the parameters were (re)set: U_K^-1 re-tiled into the contiguous K-major panels the tensor cores read
-    unsigned char* dst = c->pool + c->off.prep_uinvT + (size_t)layer * c->dims.d_kv * c->dims.d_kv * 2;
-    if (launch_uinv_panels(c->params[layer].Uinv_k, dst, c->dims.d_kv, (cudaStream_t)stream) != cudaSuccess) return TWKV_ERR_CUDA;
-    // box = a whole panel for the single-CTA kernel, the CTA's half of its rows for the pair kernel
-    if (!make_tmap_2d(&c->map_uinvT[layer], dst, (uint64_t)c->dims.NC * c->dims.d_kv, PANEL, PANEL * 2,
-                      c->kscore_pairs ? HEAD_DIM / 2 : HEAD_DIM)) return TWKV_ERR_CUDA;
-    c->prepared[layer] = !is_capturing((cudaStream_t)stream);      // (as for the gate weights)
-  }
+  if (!prepare_uinv(c, layer, (cudaStream_t)stream)) return TWKV_ERR_CUDA;
   TcMaps maps;
   maps.blocks = c->map_blocks;
   maps.boxes = c->map_boxes;
@@ -935,9 +940,12 @@ twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* 
   if (group == 0) return TWKV_ERR_CAPACITY;
   DeviceGuard g(c->device);
   if (!g.ok) return TWKV_ERR_CUDA;
+  const int n_pieces = tree_max_pairs(c->sm_count);
+  if (n_pieces == 0) return TWKV_ERR_UNSUPPORTED;                  // the score kernel runs on CTA pairs only
   ProfBind pb(&c->prof);
   cudaStream_t st = (cudaStream_t)stream;
-  const int n_pieces = c->sm_count / 2;
+  if (!prepare_uinv(c, layer, st)) return TWKV_ERR_CUDA;
+  const DevView& v = c->view;
   for (int r0 = 0; r0 < n_req; r0 += group) {
     TreeCall a = tree_shape(c, std::min(group, n_req - r0), max_nodes);
     tree_layout(c, a, (unsigned char*)workspace);
@@ -945,7 +953,15 @@ twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* 
     a.req_seqs = req_seqs; a.offsets = offsets; a.positions = positions; a.masks = (const unsigned long long*)masks;
     a.out = out; a.n_rows = n_rows; a.r0 = r0;
     if (launch_tree_plan(c->view, a, layer, n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
-    if (launch_tree_score(c->view, a, layer, c->params[layer], n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
+    TreeMaps maps;
+    maps.blocks = c->map_blocks;
+    maps.boxes = c->map_boxes;
+    const uint64_t node_rows = (uint64_t)a.n_req * v.NC * TREE_PANEL_ROWS;
+    a.q_box = tree_query_box(a);
+    if (!make_tmap_2d(&maps.nodes, a.nk, node_rows, PANEL, PANEL * 2, TILE) || !make_tmap_2d(&maps.node_boxes, a.nv, node_rows, PANEL, PANEL * 2, JOINT_ROWS) ||
+        !make_tmap_2d(&maps.uinvT, c->pool + c->off.prep_uinvT + (size_t)layer * v.d_kv * v.d_kv * 2, (uint64_t)v.NC * v.d_kv, PANEL, PANEL * 2, HEAD_DIM / 2) ||
+        !make_tmap_2d(&maps.q, a.qop, (uint64_t)a.n_req * v.Hkv * a.Rp, HEAD_DIM, HEAD_DIM * 2, (uint32_t)a.q_box)) return TWKV_ERR_CUDA;
+    if (launch_tree_score(v, a, maps, layer, n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
     if (launch_tree_value(c->view, a, st) != cudaSuccess) return TWKV_ERR_CUDA;
     if (launch_tree_merge(c->view, a, c->params[layer], st) != cudaSuccess) return TWKV_ERR_CUDA;
   }

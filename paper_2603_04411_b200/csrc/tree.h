@@ -31,6 +31,7 @@ struct TreeCall {
   int C;                // columns of a score row, Hkv Rs
   int n_splits;
   int entries;          // room of a request in the K list
+  int q_box;            // rows of qop that a CTA takes at a time
   // workspace
   unsigned short* qop;  // [n_req][Hkv][Rp][128] f16 queries in the order of the score contraction
   unsigned char *nk, *nv;     // [n_req][NC][64 rows][64] panels of the nodes' keys and values
@@ -45,6 +46,9 @@ struct TreeCall {
   float* part_acc;      // [n_req][T][n_splits][Hq][d_kv]
   float* part_l;        // [n_req][T][n_splits][Hq]
 };
+
+// The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the queries.
+struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q; };
 
 // Rows of tree i; false where the offsets do not describe at most max_nodes rows of n_rows.
 __device__ __forceinline__ bool tree_rows(const int* offsets, int i, int n_rows, int max_nodes, int* first, int* n) {
@@ -62,7 +66,9 @@ cudaError_t launch_tree_map(const DevView& v, const int* offsets, const int* par
 cudaError_t launch_tree_accept(const DevView& v, const int* offsets, const int* parents, const int* draft, const int* target, int n_req, int n_rows,
                                int max_nodes, int* n_accepted, int* rows, int* next_tokens, cudaStream_t st);
 cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int n_pieces, cudaStream_t st);
-cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, int layer, const LayerParams& lp, int n_pieces, cudaStream_t st);
+cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, const TreeMaps& maps, int layer, int n_pieces, cudaStream_t st);
+int tree_max_pairs(int sm_count);
+int tree_query_box(const TreeCall& a);
 cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, cudaStream_t st);
 cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const LayerParams& lp, cudaStream_t st);
 

@@ -1,7 +1,7 @@
 // Attention of drafted trees over the mixed-rank cache: scores, weighted values, projection.
 //
 //   tree_plan_kernel (tree_plan.cu)  lists, splits, links, the nodes' states and the queries as operands
-//   tree_score_kernel   per K tile and KV head: keys rebuilt and rotated (Eq. 3), scores with all query rows of the request
+//   tree_score_kernel (tree_score.cu)  per K tile and KV head: keys rebuilt and rotated (Eq. 3), scores with all query rows of the request
 //   tree_value_kernel   per (request, split): sum of exp(s - max) X^_V in spectral space, and the sum of the weights
 //   tree_merge_kernel   sum of the splits, projection by U_V^-1
 #include "twkv_dev.h"
@@ -9,91 +9,6 @@
 #include "tree.h"
 
 namespace twkv {
-
-constexpr int TS_THREADS = 256;
-constexpr size_t TS_SMEM = (size_t)TILE * (HEAD_DIM + 1) * sizeof(float);
-
-// One unit = (K list entry, KV head).  A thread rebuilds half of a token's dimensions (32 hf .. + 31 and the 32 that are 64 above them).
-template <bool BF16>
-__global__ void __launch_bounds__(TS_THREADS) tree_score_kernel(DevView v, TreeCall a, int layer, const unsigned short* U, int n_pieces) {
-  extern __shared__ float s_k[];                           // [128][129]
-  __shared__ int s_row[TILE];                              // score row, -1: no token
-  chain_start();
-  chain_wait();
-  const int tid = threadIdx.x, row = tid & 127, hf = tid >> 7;
-  const int n_units = a.cta_start[n_pieces] / *a.parts * 2 * v.Hkv;
-  for (int u = blockIdx.x; u < n_units; u += gridDim.x) {
-    const int4 e = a.klist[u / v.Hkv];
-    const int g = u % v.Hkv, cls = e.y & TREE_CLASS, n_valid = e.y >> 16;
-    if (e.y & TREE_FILLER) continue;
-    const bool node = (e.y & TREE_NODES) != 0;
-    const int4 info = a.info[e.w];
-    const unsigned char* src = nullptr;
-    int out_row = -1, pos = 0, panels = cls;
-    size_t panel_bytes = BLOCK_BYTES;
-    if (node) {
-      if (row < n_valid) {
-        out_row = e.x * TILE + row;
-        pos = a.positions[info.x + row];
-        src = a.nk + ((size_t)e.z + row) * (PANEL * 2);
-        panel_bytes = TREE_PANEL_ROWS * PANEL * 2;
-      }
-    } else {
-      const int slot = e.x < 0 ? v.joint_rows()[(size_t)~e.x * TILE + row] : (row < n_valid ? e.x * TILE + row : -1);
-      if (slot >= 0) {
-        out_row = v.kv_link[slot];
-        pos = v.aux(layer, 0)[slot];
-        const int4 d = v.desc(layer, 0)[slot / TILE];
-        panels = d.y;
-        src = v.blocks + (size_t)d.w * BLOCK_BYTES + (slot % TILE) * (PANEL * 2);
-      }
-    }
-    float lo[32], hi[32];
-#pragma unroll
-    for (int k = 0; k < 32; ++k) lo[k] = hi[k] = 0.f;
-    if (out_row >= 0)
-      for (int j = 0; j < panels * PANEL; ++j) {
-        const float x = to_f32<BF16>(reinterpret_cast<const unsigned short*>(src + (size_t)(j / PANEL) * panel_bytes)[j % PANEL]);
-        const unsigned short* w = U + (size_t)j * v.d_kv + g * HEAD_DIM + hf * 32;
-#pragma unroll
-        for (int k = 0; k < 32; ++k) {
-          lo[k] += x * to_f32<BF16>(w[k]);
-          hi[k] += x * to_f32<BF16>(w[64 + k]);
-        }
-      }
-#pragma unroll
-    for (int k = 0; k < 32; ++k) {
-      const int f = hf * 32 + k;
-      const float4 th = v.rope_hi[(size_t)((pos >> 4) & (ROPE_HI - 1)) * 32 + f / 2], tl = v.rope_lo[(pos & 15) * 32 + f / 2];
-      const float ch = f & 1 ? th.y : th.x, sh = f & 1 ? th.w : th.z, cl = f & 1 ? tl.y : tl.x, sl = f & 1 ? tl.w : tl.z;
-      const float c = ch * cl - sh * sl, s = sh * cl + ch * sl;
-      s_k[row * (HEAD_DIM + 1) + f] = lo[k] * c - hi[k] * s;
-      s_k[row * (HEAD_DIM + 1) + 64 + f] = hi[k] * c + lo[k] * s;
-    }
-    if (hf == 0) s_row[row] = out_row;
-    __syncthreads();
-    for (int x = tid; x < a.R * TILE; x += TS_THREADS) {
-      const int n = x / TILE, rw = x % TILE, t = n / v.rep;
-      float s = -INFINITY;
-      if (s_row[rw] >= 0) {
-        if (t < info.y && (!node || (a.masks[info.x + t] >> rw & 1ull))) {
-          const unsigned short* qq = a.qop + (((size_t)e.w * v.Hkv + g) * a.Rp + n) * HEAD_DIM;
-          s = 0.f;
-          for (int k = 0; k < HEAD_DIM; ++k) {
-            const int kc = k >> 3, ch = (kc >> 3) * 4 + ((kc & 7) >> 1) + 8 * (kc & 1);
-            s += to_f32<false>(qq[k]) * s_k[rw * (HEAD_DIM + 1) + ch * 8 + (k & 7)];
-          }
-          s *= v.sm_scale;
-        }
-        a.scores[(size_t)s_row[rw] * a.C + g * a.Rs + n] = s;
-      }
-      unsigned m = enc_ordered(s);
-      for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if ((tid & 31) == 0) atomicMax(&a.seqmax[(size_t)e.w * a.C + g * a.Rs + n], m);
-    }
-    __syncthreads();
-  }
-}
 
 // CTA = (request, split; 64 score columns; panel of 64 components).
 template <bool BF16>
@@ -161,16 +76,6 @@ __global__ void __launch_bounds__(128) tree_merge_kernel(DevView v, TreeCall a, 
   else reinterpret_cast<unsigned short*>(a.out)[at] = from_f32<false>(o);
 }
 
-cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, int layer, const LayerParams& lp, int n_pieces, cudaStream_t st) {
-  ProfScope ps(TWKV_K_KSCORE, st);
-  auto kernel = v.dtype == TWKV_BF16 ? tree_score_kernel<true> : tree_score_kernel<false>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TS_SMEM);
-  if (e != cudaSuccess) return e;
-  e = launch_chained(kernel, dim3(296), dim3(TS_THREADS), dim3(1), TS_SMEM, st, v, a, layer, reinterpret_cast<const unsigned short*>(lp.Uinv_k), n_pieces);
-  if (e != cudaSuccess) return e;
-  count_launch();
-  return cudaGetLastError();
-}
 cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, cudaStream_t st) {
   ProfScope ps(TWKV_K_VACC, st);
   auto kernel = v.dtype == TWKV_BF16 ? tree_value_kernel<true> : tree_value_kernel<false>;
