@@ -69,7 +69,7 @@ cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int
 cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, const TreeMaps& maps, int layer, int n_pieces, cudaStream_t st);
 int tree_max_pairs(int sm_count);
 int tree_query_box(const TreeCall& a);
-cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, cudaStream_t st);
+cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);
 cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const LayerParams& lp, cudaStream_t st);
 
 }  // namespace twkv
