@@ -960,10 +960,11 @@ twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* 
     a.q_box = tree_query_box(a);
     if (!make_tmap_2d(&maps.nodes, a.nk, node_rows, PANEL, PANEL * 2, TILE) || !make_tmap_2d(&maps.node_boxes, a.nv, node_rows, PANEL, PANEL * 2, JOINT_ROWS) ||
         !make_tmap_2d(&maps.uinvT, c->pool + c->off.prep_uinvT + (size_t)layer * v.d_kv * v.d_kv * 2, (uint64_t)v.NC * v.d_kv, PANEL, PANEL * 2, HEAD_DIM / 2) ||
-        !make_tmap_2d(&maps.q, a.qop, (uint64_t)a.n_req * v.Hkv * a.Rp, HEAD_DIM, HEAD_DIM * 2, (uint32_t)a.q_box)) return TWKV_ERR_CUDA;
+        !make_tmap_2d(&maps.q, a.qop, (uint64_t)a.n_req * v.Hkv * a.Rp, HEAD_DIM, HEAD_DIM * 2, (uint32_t)a.q_box) ||
+        !make_tmap_2d(&maps.uv, c->params[layer].Uinv_v, (uint64_t)v.d_kv, (uint64_t)v.d_kv, (uint64_t)v.d_kv * 2, (uint32_t)v.d_kv / 8)) return TWKV_ERR_CUDA;
     if (launch_tree_score(v, a, maps, layer, n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
     if (launch_tree_value(v, a, maps, st) != cudaSuccess) return TWKV_ERR_CUDA;
-    if (launch_tree_merge(c->view, a, c->params[layer], st) != cudaSuccess) return TWKV_ERR_CUDA;
+    if (launch_tree_merge(v, a, maps, st) != cudaSuccess) return TWKV_ERR_CUDA;
   }
   return TWKV_OK;
 }

@@ -37,7 +37,7 @@ struct TreeCall {
   unsigned char *nk, *nv;     // [n_req][NC][64 rows][64] panels of the nodes' keys and values
   unsigned* seqmax;     // [n_req][C]
   float* scores;        // [n_req][TPS + 1][128][C]
-  int4* info;           // [n_req] first row, nodes, sequence (-1: refused), V tiles of the sequence
+  int4* info;           // [n_req] first row, nodes, sequence (-1: refused), splits that hold tiles
   unsigned long long* bad;    // [n_req] nodes whose values are not finite
   int4* klist;          // entries of all requests, a request's from an even place on
   int4* vmeta;          // [n_req][TPS + 1] V tiles in stride order: score tile, class, tokens, first block (-1: the nodes)
@@ -47,8 +47,9 @@ struct TreeCall {
   float* part_l;        // [n_req][T][n_splits][Hq]
 };
 
-// The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the queries.
-struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q; };
+// The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the
+// queries, U_V^-1 (an eighth of its rows, 64 columns).
+struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q, uv; };
 
 // Rows of tree i; false where the offsets do not describe at most max_nodes rows of n_rows.
 __device__ __forceinline__ bool tree_rows(const int* offsets, int i, int n_rows, int max_nodes, int* first, int* n) {
@@ -70,6 +71,6 @@ cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, const TreeMap
 int tree_max_pairs(int sm_count);
 int tree_query_box(const TreeCall& a);
 cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);
-cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const LayerParams& lp, cudaStream_t st);
+cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);
 
 }  // namespace twkv

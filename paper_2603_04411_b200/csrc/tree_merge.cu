@@ -1,0 +1,192 @@
+// End of tree attention: sum of the splits, division by the sum of the weights, projection out_h = (acc_h / l_h) U_V^-1[:, head slice].
+//
+// A cluster of eight CTAs per (128 rows, KV head): row = (request, node; head of the group), and CTA c takes the spectral components
+// [c d/8, (c + 1) d/8).  It sums their splits, normalises, and makes them the A operand of a tcgen05 product with its rows of U_V^-1
+// (as they lie: MN-major B): two 16-bit parts of the cache type per component, fp32 accumulation in tensor memory.  The eight partial
+// products meet in distributed shared memory, 16 columns per CTA.  What bounds it is the way of the partial sums (4 d_kv bytes per row and
+// split) into the SMs, and for few rows the chain of reads; the decode merge does the product by FMAs, which for hundreds of nodes cost
+// several times the reads (256 nodes of 32 heads 373 us by a CTA per row).
+// chain_start() stands behind the allocation of tensor memory: two CTAs of this kernel share an SM, so the next kernel of the chain must
+// not find columns free that one of them still needs.
+#include "twkv_dev.h"
+#include "tc_util.cuh"
+#include "mma_util.cuh"
+#include "tree.h"
+
+namespace twkv {
+using namespace tc;
+
+constexpr int TM_THREADS = 256, TM_CL = 8;
+constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 components] of one part
+constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // high and low parts of up to 128 components; their rows of U_V^-1, 128 columns
+constexpr uint32_t TM_SMEM = TM_A + TM_B + 64;
+static_assert(TM_CL * TILE * (HEAD_DIM / TM_CL) * 4 <= TM_A, "the partial products arrive where the A operand was");
+
+template <bool BF16>
+__global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
+  const uint32_t b_full = sB + TM_B, done = b_full + 8;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + TM_A + TM_B + 16);
+  volatile int* abort_flag = reinterpret_cast<int*>(s_tmem + 1);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int c = (int)cluster_cta_rank(), g = blockIdx.y, rep = v.rep, jn = v.d_kv / TM_CL, j0 = c * jn;      // jn: a multiple of 16, at most 128
+  const int slot0 = (blockIdx.x / TM_CL) * (TILE / rep), n_slots = a.n_req * a.T;
+  const bool misaligned = (sA & 1023u) != 0;
+  if (tid == 0) {
+    mbar_init(b_full, 1);
+    mbar_init(done, 1);
+    *abort_flag = misaligned ? 1 : 0;
+    mbar_init_fence();
+  }
+  if (warp == 1) tmem_alloc(smem_addr(s_tmem), 128);
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  chain_start();
+  const uint32_t tmem = *s_tmem;
+  chain_wait();
+  if (warp == 0 && elect_one() && !misaligned) {               // on its way while the splits are summed
+    mbar_expect_tx(b_full, (uint32_t)jn * 256u);
+    tma_load_2d(sB, &map_uv, b_full, g * HEAD_DIM, j0);
+    tma_load_2d(sB + jn * 128u, &map_uv, b_full, g * HEAD_DIM + 64, j0);
+  }
+  __syncwarp();
+
+  // rows: a warp each, its lanes four components; row (slot, h), slot = request * T + node
+  auto row_at = [&](int r, int& req, int& t) -> bool {
+    const int slot = slot0 + r / rep;
+    req = slot / a.T;
+    t = slot - req * a.T;
+    return slot < n_slots && t < a.info[req].y;
+  };
+  const size_t stride = (size_t)v.Hq * v.d_kv / 4;              // float4 from split to split
+  for (int r = warp; r < TILE; r += TM_THREADS / 32) {
+    int req, t;
+    if (!row_at(r, req, t)) continue;
+    const int used = a.info[req].w;                             // splits that hold something come first
+    const size_t row = (size_t)(req * a.T + t) * a.n_splits * v.Hq + g * rep + r % rep;
+    const int* cut = a.vcut + (size_t)req * (a.n_splits + 1);
+    float l = 0.f;
+    for (int s0 = 0; s0 < used; s0 += 32) {
+      const float mine = s0 + lane < used ? a.part_l[row + (size_t)(s0 + lane) * v.Hq] : 0.f;
+      const int n = min(32, used - s0);
+      for (int s = 0; s < n; ++s) l += __shfl_sync(0xffffffffu, mine, s);
+    }
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (lane * 4 < jn) {
+      const float4* p = reinterpret_cast<const float4*>(a.part_acc + row * v.d_kv + j0) + lane;
+      for (int s0 = 0; s0 < used; s0 += 8) {
+        float4 y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          y[k] = s0 + k < used && cut[s0 + k + 1] > cut[s0 + k] ? p[(size_t)(s0 + k) * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { x.x += y[k].x; x.y += y[k].y; x.z += y[k].z; x.w += y[k].w; }
+      }
+      const float il = l == 0.f ? 0.f : 1.f / l;                // 0: no token seen; a NaN stays one
+      uint32_t hi[2], lo[2];
+      uint64_t w;
+      asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.x * il), "f"(x.y * il));
+      split_pair_16<BF16>(w, hi[0], lo[0]);
+      asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.z * il), "f"(x.w * il));
+      split_pair_16<BF16>(w, hi[1], lo[1]);
+      const int comp = lane * 4;
+      unsigned char* d = smem + (comp >> 6) * TM_PANEL + r * 128 + ((((comp >> 3) & 7) ^ (r & 7)) << 4) + (comp & 7) * 2;
+      *reinterpret_cast<uint2*>(d) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(d + 2 * TM_PANEL) = make_uint2(lo[0], lo[1]);
+    }
+  }
+  fence_proxy_async_smem();
+  __syncthreads();
+  bool ok = !misaligned;
+  if (warp == 0 && elect_one() && ok) {
+    if (mbar_wait(b_full, 0u, abort_flag)) {
+      fence_after_sync();
+      constexpr uint32_t idesc = idesc_f16(BF16 ? 1 : 0, 128, 128) | (1u << 16);       // B MN-major
+      const uint32_t b_lo = ((sB >> 4) & 0x3fffu) | ((uint32_t)(jn * 128) >> 4 << 16);
+      for (int part = 1; part >= 0; --part)                     // the low parts first: the sum is cut after every instruction
+        for (int ks = 0; ks < jn / 16; ++ks) {
+          const uint32_t a_lo = kmajor_sw128_desc_lo(sA + part * 2 * TM_PANEL + (ks >> 2) * TM_PANEL) + 2 * (ks & 3);
+          mma_f16_ss(tmem, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | a_lo, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u), idesc,
+                     part == 0 || ks > 0 ? 1u : 0u);
+        }
+      mma_commit(done);
+    }
+  }
+  __syncwarp();
+  ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag));
+  fence_after_sync();
+  cluster_sync_all();                                           // every CTA's A operand has been used: the parts may arrive there
+  {
+    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+    float x[32];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int col = half * 64 + k * 32;
+      if (ok) {
+        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + col, x);
+        tmem_ld_wait();
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) x[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 32; e += 4)                           // to the CTA that writes these columns
+        st_cluster_f32x4(cluster_map(sA + (uint32_t)((c * TILE + row) * 64 + (e & 15) * 4), (uint32_t)((col + e) >> 4)), make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
+    }
+  }
+  fence_before_sync();
+  cluster_sync_all();                                           // every part has arrived; nothing remote is touched from here on
+  fence_after_sync();
+  if (warp == 1) tmem_dealloc(tmem, 128);
+  {
+    const int r = tid >> 1, e0 = (tid & 1) * 8;
+    int req, t;
+    if (row_at(r, req, t)) {
+      const float* in = reinterpret_cast<const float*>(smem) + r * 16 + e0;
+      float o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll
+      for (int k = 0; k < TM_CL; ++k) {                         // fixed order
+        const float4 x = *reinterpret_cast<const float4*>(in + k * TILE * 16), y = *reinterpret_cast<const float4*>(in + k * TILE * 16 + 4);
+        o[0] += x.x; o[1] += x.y; o[2] += x.z; o[3] += x.w; o[4] += y.x; o[5] += y.y; o[6] += y.z; o[7] += y.w;
+      }
+      const int4 info = a.info[req];
+      if (info.z >= 0 && (a.masks[info.x + t] & a.bad[req])) {  // sees a node whose value is not finite
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = __int_as_float(0x7fffffff);
+      }
+      const size_t at = ((size_t)(info.x + t) * v.Hq + g * rep + r % rep) * HEAD_DIM + c * 16 + e0;
+      if (v.out_dtype == TWKV_F32) {
+        float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at);
+        d[0] = make_float4(o[0], o[1], o[2], o[3]);
+        d[1] = make_float4(o[4], o[5], o[6], o[7]);
+      } else {
+        unsigned w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (v.out_dtype == TWKV_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(o[2 * k + 1]), "f"(o[2 * k]));
+          else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(o[2 * k + 1]), "f"(o[2 * k]));
+        }
+        *reinterpret_cast<uint4*>(reinterpret_cast<unsigned short*>(a.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  if (tid == 0 && *abort_flag) set_status(v, misaligned ? TWKV_ERR_DEVICE_CHECK : TWKV_ERR_TIMEOUT);
+}
+
+cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
+  ProfScope ps(TWKV_K_MERGE, st);
+  auto kernel = v.dtype == TWKV_BF16 ? tree_merge_kernel<true> : tree_merge_kernel<false>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TM_SMEM);
+  if (e != cudaSuccess) return e;
+  const int tiles = (a.n_req * a.T * v.rep + TILE - 1) / TILE;
+  e = launch_chained(kernel, dim3(TM_CL * tiles, v.Hkv), dim3(TM_THREADS), dim3(TM_CL), TM_SMEM, st, maps.uv, v, a);
+  if (e != cudaSuccess) return e;
+  count_launch();
+  return cudaGetLastError();
+}
+
+}  // namespace twkv

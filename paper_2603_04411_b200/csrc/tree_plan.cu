@@ -254,7 +254,8 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
   const int tid = threadIdx.x, n_splits = a.n_splits;
   int* cut = a.vcut + (size_t)i * (n_splits + 1);
   const int nv = r.z >= 0 && r.y > 0 ? v.svc(layer)[r.z] : 0, n = r.z >= 0 && r.y > 0 ? nv + 1 : 0;
-  if (tid == 0) a.info[i] = make_int4(r.x, r.y, r.z, nv);
+  const int used = n > 0 ? min(n_splits, max(1, n / 4)) : 0;
+  if (tid == 0) a.info[i] = make_int4(r.x, r.y, r.z, used);
   if (n == 0) {
     for (int s = tid; s <= n_splits; s += 1024) cut[s] = 0;
     return;
@@ -282,7 +283,6 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
     block_scan_excl(cost(k0 + tid), s_warp, &part);
     total += part;
   }
-  const int used = min(n_splits, max(1, n / 4));
   const unsigned long long W = (unsigned long long)total, ns = (unsigned long long)used;
   int base = 0;
   for (int k0 = 0; k0 < n; k0 += 1024) {
