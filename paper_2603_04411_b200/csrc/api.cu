@@ -848,15 +848,15 @@ static size_t tree_layout(const twkv_cache* c, TreeCall& a, unsigned char* base)
   a.nk = take(n * v.NC * TREE_PANEL_ROWS * PANEL * 2);
   a.nv = take(n * v.NC * TREE_PANEL_ROWS * PANEL * 2);
   a.qop = (unsigned short*)take(n * v.Hkv * a.Rp * HEAD_DIM * 2);
-  a.seqmax = (unsigned*)take(n * a.C * sizeof(unsigned));
   a.info = (int4*)take(n * sizeof(int4));
   a.bad = (unsigned long long*)take(n * sizeof(unsigned long long));
+  a.seers = (unsigned long long*)take(n * TWKV_TREE_MAX_NODES * sizeof(unsigned long long));
   a.klist = (int4*)take(n * a.entries * sizeof(int4));
   a.vmeta = (int4*)take(n * tiles * sizeof(int4));
   a.vcut = (int*)take(n * (a.n_splits + 1) * sizeof(int));
   a.cta_start = (int*)take((MAX_PLAN_CTAS + 1) * sizeof(int));
   a.parts = (int*)take(sizeof(int));
-  a.part_l = (float*)take(parts * sizeof(float));
+  a.part_ml = (float2*)take(parts * sizeof(float2));
   a.part_acc = (float*)take(parts * v.d_kv * sizeof(float));
   a.scores = (float*)take(n * tiles * TILE * a.C * sizeof(float));
   return at;
@@ -867,7 +867,7 @@ static TreeCall tree_shape(const twkv_cache* c, int n_req, int max_nodes) {
   const DevView& v = c->view;
   TreeCall a = {};
   a.n_req = n_req; a.T = max_nodes;
-  a.R = max_nodes * v.rep; a.Rs = (a.R + 3) & ~3; a.Rp = (a.R + 15) & ~15; a.C = v.Hkv * a.Rs;
+  a.R = max_nodes * v.rep; a.Rs = a.R > 4 ? (a.R + 7) & ~7 : 4; a.Rp = (a.R + 15) & ~15; a.C = v.Hkv * a.Rs;
   a.entries = (v.TPS + 4) & ~1;
   a.n_splits = std::max(1, std::min(TREE_MAX_SPLITS, c->sm_count / (n_req * ((a.C + 63) / 64))));
   return a;

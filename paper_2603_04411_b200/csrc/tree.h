@@ -2,7 +2,7 @@
 //
 // A request is a sequence and the nodes of its tree.  The nodes' own states lie in two tiles of the workspace, one of keys and one
 // of values, beside the sequence's tiles in the cache; a score row is a token's (or node's) scores with all query rows of the request:
-//   column (g Rs + t rep + h): KV head g, node t, query head h of the group; Rs = max_nodes rep rounded up to four
+//   column (g Rs + t rep + h): KV head g, node t, query head h of the group; Rs = max_nodes rep rounded up to 4, beyond 4 to 8
 // and rows lie in the order of the request's V tiles (in the order of the sequence's list, the nodes' tile behind them), 128 a tile.
 #pragma once
 #include <cuda.h>
@@ -27,7 +27,7 @@ struct TreeCall {
   // this pass: requests r0 .. r0 + n_req - 1 of the call
   int r0, n_req;
   int T;                // most nodes of a request
-  int R, Rs, Rp;        // query rows of a KV head: T rep; rounded up to 4 (score columns), to 16 (operand rows)
+  int R, Rs, Rp;        // query rows of a KV head: T rep; score columns; operand rows (R rounded up to 16)
   int C;                // columns of a score row, Hkv Rs
   int n_splits;
   int entries;          // room of a request in the K list
@@ -35,16 +35,16 @@ struct TreeCall {
   // workspace
   unsigned short* qop;  // [n_req][Hkv][Rp][128] f16 queries in the order of the score contraction
   unsigned char *nk, *nv;     // [n_req][NC][64 rows][64] panels of the nodes' keys and values
-  unsigned* seqmax;     // [n_req][C]
   float* scores;        // [n_req][TPS + 1][128][C]
   int4* info;           // [n_req] first row, nodes, sequence (-1: refused), splits that hold tiles
   unsigned long long* bad;    // [n_req] nodes whose values are not finite
+  unsigned long long* seers;  // [n_req][64] the nodes that see a node: bit t of entry k = bit k of node t's mask
   int4* klist;          // entries of all requests, a request's from an even place on
   int4* vmeta;          // [n_req][TPS + 1] V tiles in stride order: score tile, class, tokens, first block (-1: the nodes)
   int* vcut;            // [n_req][n_splits + 1]
   int *cta_start, *parts;     // [pieces + 1] first item part of a piece; parts of an item
   float* part_acc;      // [n_req][T][n_splits][Hq][d_kv]
-  float* part_l;        // [n_req][T][n_splits][Hq]
+  float2* part_ml;      // [n_req][T][n_splits][Hq] maximum of the split (powers of two), sum of its weights
 };
 
 // The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the

@@ -1,7 +1,7 @@
 // End of tree attention: sum of the splits, division by the sum of the weights, projection out_h = (acc_h / l_h) U_V^-1[:, head slice].
 //
 // A cluster of eight CTAs per (128 rows, KV head): row = (request, node; head of the group), and CTA c takes the spectral components
-// [c d/8, (c + 1) d/8).  It sums their splits, normalises, and makes them the A operand of a tcgen05 product with its rows of U_V^-1
+// [c d/8, (c + 1) d/8).  It sums their splits, each relative to its own maximum, normalises, and makes them the A operand of a tcgen05 product with its rows of U_V^-1
 // (as they lie: MN-major B): two 16-bit parts of the cache type per component, fp32 accumulation in tensor memory.  The eight partial
 // products meet in distributed shared memory, 16 columns per CTA.  What bounds it is the way of the partial sums (4 d_kv bytes per row and
 // split) into the SMs, and for few rows the chain of reads; the decode merge does the product by FMAs, which for hundreds of nodes cost
@@ -20,7 +20,10 @@ constexpr int TM_THREADS = 256, TM_CL = 8;
 constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 components] of one part
 constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // high and low parts of up to 128 components; their rows of U_V^-1, 128 columns
 constexpr uint32_t TM_SMEM = TM_A + TM_B + 64;
+static_assert(TREE_MAX_SPLITS <= 64, "two splits per lane");
 static_assert(TM_CL * TILE * (HEAD_DIM / TM_CL) * 4 <= TM_A, "the partial products arrive where the A operand was");
+
+__device__ __forceinline__ float tm_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
 template <bool BF16>
 __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
@@ -67,24 +70,36 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     const int used = a.info[req].w;                             // splits that hold something come first
     const size_t row = (size_t)(req * a.T + t) * a.n_splits * v.Hq + g * rep + r % rep;
     const int* cut = a.vcut + (size_t)req * (a.n_splits + 1);
-    float l = 0.f;
-    for (int s0 = 0; s0 < used; s0 += 32) {
-      const float mine = s0 + lane < used ? a.part_l[row + (size_t)(s0 + lane) * v.Hq] : 0.f;
-      const int n = min(32, used - s0);
-      for (int s = 0; s < n; ++s) l += __shfl_sync(0xffffffffu, mine, s);
+    // lane = split, or two: their weights relative to the largest maximum, and the sum of all weights
+    float top[2], l[2], w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float2 ml = lane + 32 * h < used ? a.part_ml[row + (size_t)(lane + 32 * h) * v.Hq] : make_float2(-INFINITY, 0.f);
+      top[h] = ml.x; l[h] = ml.y;
     }
+    float most = fmaxf(top[0], top[1]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+#pragma unroll
+    for (int h = 0; h < 2; ++h) w[h] = top[h] == -INFINITY ? 0.f : tm_ex2(top[h] - most);
+    float sum = l[0] * w[0] + l[1] * w[1];                       // (a sum that is not a number stays one)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const float il = sum == 0.f ? 0.f : 1.f / sum;               // 0: no token seen
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (lane * 4 < jn) {
-      const float4* p = reinterpret_cast<const float4*>(a.part_acc + row * v.d_kv + j0) + lane;
-      for (int s0 = 0; s0 < used; s0 += 8) {
-        float4 y[8];
+    const float4* p = reinterpret_cast<const float4*>(a.part_acc + row * v.d_kv + j0) + lane;
+    for (int s0 = 0; s0 < used; s0 += 8) {
+      float4 y[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          y[k] = s0 + k < used && cut[s0 + k + 1] > cut[s0 + k] ? p[(size_t)(s0 + k) * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = 0; k < 8; ++k)
+        y[k] = lane * 4 < jn && s0 + k < used && cut[s0 + k + 1] > cut[s0 + k] ? p[(size_t)(s0 + k) * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) { x.x += y[k].x; x.y += y[k].y; x.z += y[k].z; x.w += y[k].w; }
+      for (int k = 0; k < 8; ++k) {
+        const float ws = __shfl_sync(0xffffffffu, s0 < 32 ? w[0] : w[1], (s0 + k) & 31);
+        x.x += y[k].x * ws; x.y += y[k].y * ws; x.z += y[k].z * ws; x.w += y[k].w * ws;
       }
-      const float il = l == 0.f ? 0.f : 1.f / l;                // 0: no token seen; a NaN stays one
+    }
+    if (lane * 4 < jn) {
       uint32_t hi[2], lo[2];
       uint64_t w;
       asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.x * il), "f"(x.y * il));

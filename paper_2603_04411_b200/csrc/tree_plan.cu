@@ -4,7 +4,7 @@
 //   n_req    the tables of its joint tiles
 //   n_req vj K slot -> score row of its cached tokens
 //   n_req 2  the nodes' states cut to their ranks, as a tile of keys and a tile of values
-//   n_req qc its queries as the operand of the score products, and the running maxima
+//   n_req qc its queries as the operand of the score products
 // The K list holds a request's tiles together, from the widest class to the narrowest, in items of two: a pair of CTAs rebuilds two
 // tiles at once and multiplies them with the same queries, so both belong to one request; the narrower one's missing panels are zeros.
 // A request with an odd number of tiles ends with a filler.  Where a class's entries of a request start follows from the keys' token
@@ -337,6 +337,13 @@ __device__ void tree_pack(const DevView& v, const TreeCall& a, int i, const int4
   }
   __syncthreads();
   if (side && tid == 0) a.bad[i] = s_bad;
+  if (!side && tid < 32) {                                           // the masks turned: a lane's two nodes' masks, one ballot per node seen
+    const unsigned long long m0 = tid < r.y ? a.masks[r.x + tid] : 0ull, m1 = tid + 32 < r.y ? a.masks[r.x + tid + 32] : 0ull;
+    for (int k = 0; k < TWKV_TREE_MAX_NODES; ++k) {
+      const unsigned lo = __ballot_sync(0xffffffffu, (m0 >> k) & 1ull), hi = __ballot_sync(0xffffffffu, (m1 >> k) & 1ull);
+      if (tid == 0) a.seers[(size_t)i * TWKV_TREE_MAX_NODES + k] = (unsigned long long)hi << 32 | lo;
+    }
+  }
 }
 
 // Queries of a request as f16 rows in the order in which the rotated keys are contracted: 16-byte piece 8 hf + 2 c holds dimensions
@@ -344,8 +351,9 @@ __device__ void tree_pack(const DevView& v, const TreeCall& a, int i, const int4
 template <bool BF16>
 __device__ void tree_queries(const DevView& v, const TreeCall& a, int i, const int4& r, int part, int parts) {
   const int tid = part * 1024 + threadIdx.x, step = parts * 1024;
-  for (int c = tid; c < a.C; c += step) a.seqmax[(size_t)i * a.C + c] = 0u;
   uint4* out = reinterpret_cast<uint4*>(a.qop + (size_t)i * v.Hkv * a.Rp * HEAD_DIM);
+  // a negative scale goes into the queries, a zero one zeroes them (-inf masks need a positive factor)
+  const unsigned flip = v.sm_scale < 0.f ? 0x80008000u : 0u, keep = v.sm_scale == 0.f ? 0u : 0xffffffffu;
   bool over = false;
   for (int k = tid; k < v.Hkv * a.Rp * 16; k += step) {
     const int kc = k & 15, row = k >> 4, g = row / a.Rp, n = row - g * a.Rp, t = n / v.rep;
@@ -363,7 +371,7 @@ __device__ void tree_queries(const DevView& v, const TreeCall& a, int i, const i
       }
       w = make_uint4(o[0], o[1], o[2], o[3]);
     }
-    out[k] = w;
+    out[k] = make_uint4((w.x ^ flip) & keep, (w.y ^ flip) & keep, (w.z ^ flip) & keep, (w.w ^ flip) & keep);
   }
   if (over) set_status(v, TWKV_ERR_DEVICE_CHECK);                   // a bf16 query beyond the f16 range would be clamped
 }

@@ -5,17 +5,18 @@
 // with all query rows of the request, nodes x heads of the group, in Q_g.  A tile is rebuilt and rotated once for all of them; that is
 // what a pass of single queries per node repeats.  The kernel runs on CTA pairs (M = 256 over two tiles of ONE request, so that
 // each CTA holds half of Q_g's rows and every column of the product is wanted).  Query rows go through in blocks of 64 columns
-// (N = 16 .. 64): their operand, made by the plan kernel, streams through a ring of three stages, a block's scores land in one of two
-// accumulators and leave through shared memory, so that a token's scores are stored as whole lines.
+// (N = 16 .. 64): their operand, made by the plan kernel, streams through a ring, a block's scores land in one of two accumulators (four of 32
+// columns where that is all there is).
 //
 // Tensor memory (512 columns): slabs of rebuilt keys 3 x 128 | score accumulators 2 x 64.
 // Warp roles (512 threads, one persistent CTA per SM; registers re-divided by warpgroup):
 //   warp 0      TMA producer of U_K^-1 panels
 //   warp 1      issuer of the reconstruction products (even CTA; owns the TMEM allocation)
-//   warp 2      TMA producer of X^_K panels
-//   warp 3      issuer of the score products (even CTA), and in both CTAs the producer of the query blocks, two ahead
+//   warp 2      TMA producer of X^_K panels and of the query blocks
+//   warp 3      issuer of the score products (even CTA)
 //   warps 4-11  rotation and high / low split (thread = one token row x half of the RoPE frequencies)
-//   warps 12-15 scores out: scaled, masked (nodes), transposed through shared memory, stored, folded into the running maxima
+//   warps 12-15 scores out: masked (nodes), stored in the order of the V tiles (thread = one token row)
+// Scores are stored without their scale, which the value kernel's exponents carry (a negative scale is in the queries).
 // A class wider than eight panels runs as two passes over its panels, the second adding to the scores the first one stored.
 // All waits are bounded (tc_util.cuh); a wait that runs out ends the kernel with TWKV_ERR_TIMEOUT.
 #include "twkv_dev.h"
@@ -26,25 +27,39 @@ namespace twkv {
 using namespace tc;
 
 constexpr int TS_THREADS = 512;
-constexpr int TS_REGS_LIGHT = 56, TS_REGS_EPI = 184, TS_REGS_OUT = 80;      // 128 x 56 + 256 x 184 + 128 x 80 = 64512 of 65536
-constexpr int TS_A_SLOTS = 8, TS_B_STAGES = 3, TS_Q_STAGES = 3, TS_SLABS = 3, TS_S_SLOTS = 2;
+constexpr int TS_REGS_LIGHT = 56, TS_REGS_EPI = 184, TS_REGS_OUT = 88;      // 128 x 56 + 256 x 184 + 128 x 88 = 65536
+constexpr int TS_A_SLOTS = 8, TS_B_STAGES = 4, TS_SLABS = 3;
+constexpr int TS_Q_STAGES = 6;                                  // stages of the query ring where a block has at most 32 rows, half as many where it has 64
+constexpr int TS_S_SLOTS = 4;                                   // score accumulators of 32 columns, or half as many of 64
 constexpr uint32_t TS_PANEL = 16384, TS_B_PART = 8192, TS_B_STAGE = 2 * TS_B_PART;
 constexpr int TS_QCOLS = 64;                                    // query rows of a block, half of them in each CTA
-constexpr uint32_t TS_Q_PANEL = TS_QCOLS / 2 * 128, TS_Q_STAGE = 2 * TS_Q_PANEL;
+constexpr uint32_t TS_Q_BYTES = 3 * TS_QCOLS / 2 * 256;          // the ring: three blocks of 64 rows, this CTA's half of each
 constexpr uint32_t TS_COL_SLAB = 0, TS_COL_S = 128 * TS_SLABS;
 constexpr int TS_ROPE_STRIDE = 33;                              // float4 per row of the small RoPE table (32 + 1 against bank conflicts)
 constexpr uint32_t TS_ROPE_BYTES = ROPE_LO * TS_ROPE_STRIDE * 16;
-constexpr uint32_t TS_OUT_WARP = 32 * 128;                      // 32 token rows x 32 columns of a warp on their way out
 constexpr int TS_N_BARS = 2 * TS_A_SLOTS + 2 * TS_B_STAGES + 2 * TS_Q_STAGES + 3 * TS_SLABS + 2 * TS_S_SLOTS;
-constexpr uint32_t TS_SMEM = TS_A_SLOTS * TS_PANEL + TS_B_STAGES * TS_B_STAGE + TS_Q_STAGES * TS_Q_STAGE + 4 * TS_OUT_WARP + TS_ROPE_BYTES + 8 * TS_N_BARS + 16;
+constexpr uint32_t TS_SMEM = TS_A_SLOTS * TS_PANEL + TS_B_STAGES * TS_B_STAGE + TS_Q_BYTES + TS_ROPE_BYTES + 8 * TS_N_BARS + 16;
 static_assert(TS_SMEM > CHAIN_TMEM_SMEM && TS_SMEM <= 232448, "no other CTA with tensor memory beside this one");
-static_assert(TS_COL_S + TS_QCOLS * TS_S_SLOTS <= 512, "tensor memory");
+static_assert(TS_COL_S + TS_QCOLS / 2 * TS_S_SLOTS <= 512, "tensor memory");
 
 __device__ __forceinline__ uint64_t ts_pack(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ uint64_t ts_pack_bits(uint32_t a, uint32_t b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b)); return r; }
 __device__ __forceinline__ uint64_t ts_mul(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ uint64_t ts_sub(uint64_t a, uint64_t b) { uint64_t r; asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ uint64_t ts_fma(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// Whether the phase has completed, without waiting for it.
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+// Looks at both rings without finding room after which the producer gives up: a look takes a few dozen cycles, so a second or more.
+constexpr uint32_t TS_IDLE_LIMIT = 1u << 26;
 
 // A work unit: this CTA's list entry, and the class of the pair (that of its wider tile, the even CTA's).
 struct TsUnit {
@@ -63,9 +78,8 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   const uint32_t sA = smem_addr(smem_raw);
   const bool misaligned = (sA & 1023u) != 0;
   const uint32_t sB = sA + TS_A_SLOTS * TS_PANEL, sQ = sB + TS_B_STAGES * TS_B_STAGE;
-  unsigned char* out_stage = smem_raw + TS_A_SLOTS * TS_PANEL + TS_B_STAGES * TS_B_STAGE + TS_Q_STAGES * TS_Q_STAGE;
-  float4* sRope = reinterpret_cast<float4*>(out_stage + 4 * TS_OUT_WARP);
-  unsigned char* tail = out_stage + 4 * TS_OUT_WARP + TS_ROPE_BYTES;
+  float4* sRope = reinterpret_cast<float4*>(smem_raw + TS_A_SLOTS * TS_PANEL + TS_B_STAGES * TS_B_STAGE + TS_Q_BYTES);
+  unsigned char* tail = reinterpret_cast<unsigned char*>(sRope) + TS_ROPE_BYTES;
   const uint32_t bars = smem_addr(tail);
   // In the even CTA, also for the odd one's copies and arrivals: a_full, b_full, q_full, kr_full, slab_empty, s_empty.  In both, signalled
   // together by a multicast commit: a_empty, b_empty, q_empty, slab_full, s_full.
@@ -100,6 +114,8 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   const int w0 = a.cta_start[piece], total = a.cta_start[piece + 1];
   const int hs = __ffs(*a.parts) - 1, nh = v.Hkv >> hs;
   const int n_sub = (a.Rp + TS_QCOLS - 1) / TS_QCOLS;
+  const uint32_t s_cols = a.Rp <= TS_QCOLS / 2 ? TS_QCOLS / 2 : TS_QCOLS, s_slots = a.Rp <= TS_QCOLS / 2 ? TS_S_SLOTS : TS_S_SLOTS / 2;
+  const uint32_t q_stages = a.Rp <= TS_QCOLS / 2 ? TS_Q_STAGES : TS_Q_STAGES / 2, q_stage = TS_Q_BYTES / q_stages, q_panel = q_stage / 2;
   auto unit = [&](int w) -> TsUnit {
     TsUnit u;
     if (w < total) {
@@ -128,40 +144,65 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   } else if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TS_REGS_LIGHT));
     if (warp == 2) {
-      // ----------------------------------------------------------- TMA producer: X^_K panels
+      // ----------------------------------------------------------- TMA producer: X^_K panels and query blocks
+      // Two queues of copies with a ring each, in the order of their use; one thread looks at the rings in turn and issues what has
+      // room, so that neither waits for the other.  (A producer of the blocks inside the issuer of their products cost that thread a
+      // quarter of its time, one inside the warps that store the scores their registers.)
       if (elect_one()) {
         tma_prefetch_desc(&map_blocks);
         tma_prefetch_desc(&map_boxes);
         tma_prefetch_desc(&map_nodes);
-        uint32_t ak = 0;                                        // panels so far; slot = ak % 8
-        bool ok = true;
-        TsUnit u = unit(w0);
-        for (int w = w0; w < total && ok; ++w) {
-          const TsUnit nxt = unit(w + 1);
-          const int own = u.e.y & TREE_CLASS;
-          const bool joint = u.e.x < 0, node = (u.e.y & TREE_NODES) != 0;
-          unsigned box[TILE / JOINT_ROWS];
-          if (joint) {
-            const uint4* b4 = reinterpret_cast<const uint4*>(v.joint_boxes() + (size_t)~u.e.x * (TILE / JOINT_ROWS));
-            const uint4 lo = b4[0], hi = b4[1];
-            box[0] = lo.x; box[1] = lo.y; box[2] = lo.z; box[3] = lo.w; box[4] = hi.x; box[5] = hi.y; box[6] = hi.z; box[7] = hi.w;
-          }
-          for (int j = 0; j < u.cls; ++j, ++ak) {
-            const uint32_t slot = ak % TS_A_SLOTS, ph = (ak / TS_A_SLOTS) & 1u, dst = sA + slot * TS_PANEL;
-            if (!(ok = mbar_wait_thin(a_empty + 8 * slot, ph ^ 1u, abort_flag))) break;
+        tma_prefetch_desc(&map_q);
+        // panels: unit w, panel j, panels so far ak (slot = ak % 8); blocks: unit lw, first panel of the pass lp, KV head lsl, block lsub
+        int w = w0, j = 0, lw = w0, lp = 0, lsl = 0, lsub = 0;
+        uint32_t ak = 0, lst = 0, lph = 0, idle = 0;
+        TsUnit u = unit(w0), lu = u;
+        while (w < total || lw < total) {
+          bool moved = false;
+          if (w < total && mbar_test(a_empty + 8 * (ak % TS_A_SLOTS), ((ak / TS_A_SLOTS) & 1u) ^ 1u)) {
+            const uint32_t slot = ak % TS_A_SLOTS, dst = sA + slot * TS_PANEL;
+            const int own = u.e.y & TREE_CLASS;
             if (crank == 0) mbar_expect_tx(a_full + 8 * slot, 2 * TS_PANEL);            // this CTA's copy and the partner's
-            if (joint) {
+            if (u.e.x < 0) {
+              const unsigned* box = v.joint_boxes() + (size_t)~u.e.x * (TILE / JOINT_ROWS);
 #pragma unroll
-              for (int b = 0; b < TILE / JOINT_ROWS; ++b)       // a box of a narrower class lies behind the last block from its class on and reads zeros there
+              for (int b = 0; b < TILE / JOINT_ROWS; ++b) {     // a box of a narrower class lies behind the last block from its class on and reads zeros there
+                const unsigned x = box[b];
                 tma_load_2d_pair(dst + b * (JOINT_ROWS * PANEL * 2), &map_boxes, a_full_even + 8 * slot, 0,
-                                 j < (int)(box[b] & 31u) ? (int)(box[b] >> 5) * JOINT_ROWS + j * TILE : v.n_blocks * TILE);
-            } else if (node && j < own) {
+                                 j < (int)(x & 31u) ? (int)(x >> 5) * JOINT_ROWS + j * TILE : v.n_blocks * TILE);
+              }
+            } else if ((u.e.y & TREE_NODES) && j < own) {
               tma_load_2d_pair(dst, &map_nodes, a_full_even + 8 * slot, 0, u.e.z + j * TREE_PANEL_ROWS);       // rows past the nodes': other panels, dropped
             } else {
               tma_load_2d_pair(dst, &map_blocks, a_full_even + 8 * slot, 0, j < own ? (u.e.z + j) * TILE : v.n_blocks * TILE);
             }
+            ++ak;
+            if (++j == u.cls) { j = 0; u = unit(++w); }
+            moved = true;
           }
-          u = nxt;
+          if (lw < total && mbar_test(q_empty + 8 * lst, lph ^ 1u)) {
+            const int half = min(TS_QCOLS, a.Rp - lsub * TS_QCOLS) / 2;
+            const int y = (lu.e.w * v.Hkv + head(first_head(lw), lsl)) * a.Rp + lsub * TS_QCOLS + (int)crank * half;
+            if (crank == 0) mbar_expect_tx(q_full + 8 * lst, 2 * 2 * (uint32_t)a.q_box * 128u);
+            tma_load_2d_pair(sQ + lst * q_stage, &map_q, q_full_even + 8 * lst, 0, y);
+            tma_load_2d_pair(sQ + lst * q_stage + q_panel, &map_q, q_full_even + 8 * lst, PANEL, y);
+            if (++lst == q_stages) { lst = 0; lph ^= 1u; }
+            if (++lsub == n_sub) {
+              lsub = 0;
+              if (++lsl == nh) {
+                lsl = 0;
+                lp += TS_A_SLOTS;
+                if (lp >= lu.cls) { lp = 0; lu = unit(++lw); }
+              }
+            }
+            moved = true;
+          }
+          idle = moved ? 0u : idle + 1u;
+          if (!moved) __nanosleep(100);
+          if ((idle & 63u) == 63u) {
+            if (*abort_flag) break;
+            if (idle > TS_IDLE_LIMIT) { *abort_flag = 1; break; }
+          }
         }
       }
       __syncwarp();
@@ -240,67 +281,37 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
       }
       __syncwarp();
     } else {
-      // ----------------------------------------------------------- query blocks in, score products
-      if (elect_one()) {
-        tma_prefetch_desc(&map_q);
+      // ----------------------------------------------------------- issuer of the score products
+      if (crank == 0 && elect_one()) {
+        const uint32_t q_lo0 = kmajor_sw128_desc_lo(sQ);
+        uint32_t sbuf = 0, sph = 0, slot = 0, slph = 0, qst = 0, qph = 0;
         bool ok = true;
-        // The blocks in order: (unit, pass, KV head, block of 64 rows).  Block n takes ring stage n % 3 once the products of block n - 3 have retired.
-        int lw = w0, lp = 0, lsl = 0, lsub = 0;
-        uint32_t lst = 0, lph = 0;
-        TsUnit lu = unit(w0);
-        auto load = [&]() -> bool {                             // the next block; nothing once all are loaded
-          if (lw >= total) return true;
-          if (!mbar_wait_thin(q_empty + 8 * lst, lph ^ 1u, abort_flag)) return false;
-          const int half = min(TS_QCOLS, a.Rp - lsub * TS_QCOLS) / 2;
-          const int y = (lu.e.w * v.Hkv + head(first_head(lw), lsl)) * a.Rp + lsub * TS_QCOLS + (int)crank * half;
-          if (crank == 0) mbar_expect_tx(q_full + 8 * lst, 2 * 2 * (uint32_t)a.q_box * 128u);
-          tma_load_2d_pair(sQ + lst * TS_Q_STAGE, &map_q, q_full_even + 8 * lst, 0, y);
-          tma_load_2d_pair(sQ + lst * TS_Q_STAGE + TS_Q_PANEL, &map_q, q_full_even + 8 * lst, PANEL, y);
-          if (++lst == TS_Q_STAGES) { lst = 0; lph ^= 1u; }
-          if (++lsub == n_sub) {
-            lsub = 0;
-            if (++lsl == nh) {
-              lsl = 0;
-              lp += TS_A_SLOTS;
-              if (lp >= lu.cls) { lp = 0; lu = unit(++lw); }
-            }
-          }
-          return true;
-        };
-        if (crank != 0) {
-          while (ok && lw < total) ok = load();
-        } else {
-          ok = load() && load();
-          const uint32_t q_lo0 = kmajor_sw128_desc_lo(sQ);
-          uint32_t sbuf = 0, sph = 0, slot = 0, slph = 0, qst = 0, qph = 0;
-          TsUnit u = unit(w0);
-          for (int w = w0; w < total && ok; ++w) {
-            const TsUnit nxt = unit(w + 1);
-            for (int p0 = 0; p0 < u.cls && ok; p0 += TS_A_SLOTS) {
-              for (int sl = 0; sl < nh && ok; ++sl) {
-                if (!(ok = mbar_wait_thin(kr_full + 8 * sbuf, sph, abort_flag))) break;
-                const uint32_t kr = tmem_base + TS_COL_SLAB + sbuf * 128;
-                for (int sub = 0; sub < n_sub; ++sub) {
-                  if (!(ok = mbar_wait_thin(s_empty + 8 * slot, slph ^ 1u, abort_flag))) break;
-                  if (!(ok = mbar_wait_thin(q_full + 8 * qst, qph, abort_flag))) break;
-                  fence_after_sync();
-                  const uint32_t idesc_s = idesc_f16(0, 256, min(TS_QCOLS, a.Rp - sub * TS_QCOLS));
-                  const uint32_t sd = tmem_base + TS_COL_S + TS_QCOLS * slot, ql = q_lo0 + qst * (TS_Q_STAGE >> 4);
-                  // high and low f16 parts of the rotated keys into the same accumulator, the low one first
-                  mma_f16_ts_k128_cg<2>(sd, kr + 64, ql, TS_Q_PANEL >> 4, idesc_s, 0u);
-                  mma_f16_ts_k128_cg<2>(sd, kr, ql, TS_Q_PANEL >> 4, idesc_s, 1u);
-                  mma_commit_pair_both(q_empty + 8 * qst);
-                  if (sub == n_sub - 1) mma_commit_pair(slab_empty + 8 * sbuf);
-                  mma_commit_pair_both(s_full + 8 * slot);
-                  if (++slot == TS_S_SLOTS) { slot = 0; slph ^= 1u; }
-                  if (++qst == TS_Q_STAGES) { qst = 0; qph ^= 1u; }
-                  if (!(ok = load())) break;
-                }
-                if (++sbuf == TS_SLABS) { sbuf = 0; sph ^= 1u; }
+        TsUnit u = unit(w0);
+        for (int w = w0; w < total && ok; ++w) {
+          const TsUnit nxt = unit(w + 1);
+          for (int p0 = 0; p0 < u.cls && ok; p0 += TS_A_SLOTS) {
+            for (int sl = 0; sl < nh && ok; ++sl) {
+              if (!(ok = mbar_wait_thin(kr_full + 8 * sbuf, sph, abort_flag))) break;
+              const uint32_t kr = tmem_base + TS_COL_SLAB + sbuf * 128;
+              for (int sub = 0; sub < n_sub; ++sub) {
+                if (!(ok = mbar_wait_thin(s_empty + 8 * slot, slph ^ 1u, abort_flag))) break;
+                if (!(ok = mbar_wait_thin(q_full + 8 * qst, qph, abort_flag))) break;
+                fence_after_sync();
+                const uint32_t idesc_s = idesc_f16(0, 256, min(TS_QCOLS, a.Rp - sub * TS_QCOLS));
+                const uint32_t sd = tmem_base + TS_COL_S + s_cols * slot, ql = q_lo0 + qst * (q_stage >> 4);
+                // high and low f16 parts of the rotated keys into the same accumulator, the low one first
+                mma_f16_ts_k128_cg<2>(sd, kr + 64, ql, q_panel >> 4, idesc_s, 0u);
+                mma_f16_ts_k128_cg<2>(sd, kr, ql, q_panel >> 4, idesc_s, 1u);
+                mma_commit_pair_both(q_empty + 8 * qst);
+                if (sub == n_sub - 1) mma_commit_pair(slab_empty + 8 * sbuf);
+                mma_commit_pair_both(s_full + 8 * slot);
+                if (++slot == s_slots) { slot = 0; slph ^= 1u; }
+                if (++qst == q_stages) { qst = 0; qph ^= 1u; }
               }
+              if (++sbuf == TS_SLABS) { sbuf = 0; sph ^= 1u; }
             }
-            u = nxt;
           }
+          u = nxt;
         }
       }
       __syncwarp();
@@ -394,13 +405,12 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TS_REGS_OUT));
     // ------------------------------------------------------------- scores out
-    // One warp per TMEM lane quarter.  32 columns at a time: a thread reads its token row, the warp turns the block in shared memory (rows
-    // of 128 bytes, 16-byte pieces swizzled), then eight lanes hold a row and store it as whole lines; a lane meets four columns of eight
-    // rows on the way, whose maxima the warp joins.  The maxima in memory are read ahead, and only a larger one is sent there.
-    const int quarter = warp & 3, row = quarter * 32 + lane, sub_row = lane >> 3, piece4 = lane & 7;
-    const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16);
-    float4* stage = reinterpret_cast<float4*>(out_stage + quarter * TS_OUT_WARP);
-    const float sm_scale = v.sm_scale;
+    // One warp per TMEM lane quarter, thread = token row: 32 columns at a time go straight to the token's score row, in pieces of 32 bytes.  A
+    // single warp issues an instruction every five cycles or so, and a slab leaves it about 2000: this loop is kept short, the
+    // maxima are the value kernel's.  (Turned in shared memory, so that lanes share a row, with maxima by column, a block of 32 columns took
+    // 1475 cycles; sent off as TMA boxes 1900.)
+    const int quarter = warp & 3, row = quarter * 32 + lane;
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + TS_COL_S;
     const int rep_shift = __ffs(v.rep) - 1;
     uint32_t slot = 0, slph = 0;
     bool ok = true;
@@ -415,84 +425,63 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     int srow = score_row(u.e);
     for (int w = w0; w < total && ok; ++w) {
       const TsUnit nxt = unit(w + 1);
-      const int srow_next = score_row(nxt.e);
       const int passes = (u.cls + TS_A_SLOTS - 1) / TS_A_SLOTS, g0 = first_head(w);
-      const bool node = (u.e.y & TREE_NODES) != 0, drop = (u.e.y & TREE_FILLER) != 0;
-      const int4 info = node ? a.info[u.e.w] : make_int4(0, 0, 0, 0);
-      int dst_row[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) dst_row[k] = __shfl_sync(0xffffffffu, srow, 4 * k + sub_row);
+      const bool live = srow >= 0;                                 // (a filler's rows are not)
+      float* const dst_row = a.scores + (size_t)(live ? srow : 0) * a.C;
+      const bool node = (u.e.y & TREE_NODES) != 0;
+      const unsigned long long seers = node ? a.seers[(size_t)u.e.w * TWKV_TREE_MAX_NODES + (row & (TWKV_TREE_MAX_NODES - 1))] : ~0ull;
+      const int srow_next = score_row(nxt.e);
       for (int ps = 0; ps < passes && ok; ++ps) {
-        const bool add = ps > 0, last = ps == passes - 1;
         for (int sli = 0; sli < nh && ok; ++sli) {
           const int g = head(g0, sli);
           for (int sub = 0; sub < n_sub; ++sub) {
-            const int cols = min(TS_QCOLS, a.Rs - sub * TS_QCOLS);             // columns to store, a multiple of four (none: only operand padding)
-            const int c_base = g * a.Rs + sub * TS_QCOLS;
-            unsigned* const top = a.seqmax + (size_t)(u.e.w) * a.C + c_base;
+            const int cols = min(TS_QCOLS, a.Rs - sub * TS_QCOLS);
+            float* const dst = dst_row + g * a.Rs + sub * TS_QCOLS;
             if (!(ok = __all_sync(0xffffffffu, mbar_wait(s_full + 8 * slot, slph, abort_flag)))) break;
             fence_after_sync();
-            const uint32_t src = lane_addr + TS_COL_S + TS_QCOLS * slot;
-            const int chunks = cols > 32 ? 2 : 1;
-            for (int ch = 0; ch < chunks; ++ch) {
-              float x[32];
+            const uint32_t src = lane_addr + s_cols * slot;
+#pragma unroll
+            for (int ch = 0; ch < 2; ++ch) {
+              if (32 * ch >= cols) break;
+              uint32_t x[32];
               tmem_ld32(src + 32 * ch, x);
-              const unsigned seen = !drop && last && 32 * ch + lane < cols ? *(volatile unsigned*)(top + 32 * ch + lane) : 0xffffffffu;
               tmem_ld_wait();
-              if (ch == chunks - 1) {
+              if (32 * ch + 32 >= cols) {                          // the accumulator has been read
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(s_empty_even + 8 * slot);
               }
-              if (drop) continue;
+              if (ps > 0 && live) {                                // what this thread stored of the first pass
 #pragma unroll
-              for (int c = 0; c < 32; ++c) x[c] *= sm_scale;
-              if (node) {                                          // a node is seen by the queries whose masks hold its bit
+                for (int c = 0; c < 4; ++c)
+                  if (32 * ch + 8 * c < cols) {
+                    const float4* p = reinterpret_cast<const float4*>(dst + 32 * ch + 8 * c);
+                    const float4 y = p[0], z = a.Rs >= 8 ? p[1] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float o[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
 #pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                  const int t = (sub * TS_QCOLS + 32 * ch + c) >> rep_shift;
-                  const unsigned long long m = t < info.y ? a.masks[info.x + t] : 0ull;
-                  if (!((m >> (row & 63)) & 1ull)) x[c] = -INFINITY;
-                }
-              }
-#pragma unroll
-              for (int c = 0; c < 8; ++c) stage[lane * 8 + (c ^ (lane & 7))] = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
-              __syncwarp();
-              const bool mine = 32 * ch + 4 * piece4 < cols;
-              float* const dst = a.scores + c_base + 32 * ch + 4 * piece4;
-              float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                const int r = 4 * k + sub_row;
-                float4 y = stage[r * 8 + (piece4 ^ (r & 7))];
-                if (mine && dst_row[k] >= 0) {
-                  float4* p = reinterpret_cast<float4*>(dst + (size_t)dst_row[k] * a.C);
-                  if (add) {                                       // (this thread stored the first pass's part)
-                    const float4 o = *p;
-                    y.x += o.x; y.y += o.y; y.z += o.z; y.w += o.w;
+                    for (int e = 0; e < 8; ++e) x[8 * c + e] = __float_as_uint(__uint_as_float(x[8 * c + e]) + o[e]);
                   }
-                  *p = y;
-                  mx[0] = fmaxf(mx[0], y.x); mx[1] = fmaxf(mx[1], y.y); mx[2] = fmaxf(mx[2], y.z); mx[3] = fmaxf(mx[3], y.w);
+              }
+              if (node) {                                          // a node is seen by the queries whose masks hold its bit
+                const unsigned bits = (unsigned)(seers >> ((sub * TS_QCOLS + 32 * ch) >> rep_shift));       // (32 columns are at most 32 nodes)
+#pragma unroll
+                for (int c = 0; c < 32; ++c)
+                  if (!((bits >> (c >> rep_shift)) & 1u)) x[c] = 0xff800000u;
+              }
+              if (live) {
+                if (a.Rs >= 8) {
+#pragma unroll
+                  for (int c = 0; c < 4; ++c)
+                    if (32 * ch + 8 * c < cols)
+                      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                                   ::"l"(__cvta_generic_to_global(dst + 32 * ch + 8 * c)), "r"(x[8 * c]), "r"(x[8 * c + 1]), "r"(x[8 * c + 2]), "r"(x[8 * c + 3]),
+                                     "r"(x[8 * c + 4]), "r"(x[8 * c + 5]), "r"(x[8 * c + 6]), "r"(x[8 * c + 7]) : "memory");
+                } else if (ch == 0) {
+                  *reinterpret_cast<uint4*>(dst) = make_uint4(x[0], x[1], x[2], x[3]);
                 }
               }
-              __syncwarp();                                        // the block has been read
-              if (!last) continue;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
-                mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
-              }
-              // lane = column: the maximum of column 4 (lane / 4) + lane % 4 sits in the lanes of piece lane / 4
-              float m = -INFINITY;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float t = __shfl_sync(0xffffffffu, mx[e], lane >> 2);
-                if ((lane & 3) == e) m = t;
-              }
-              const unsigned enc = enc_ordered(m);
-              if (enc > seen) atomicMax(top + 32 * ch + lane, enc);
             }
-            if (++slot == TS_S_SLOTS) { slot = 0; slph ^= 1u; }
+            if (++slot == s_slots) { slot = 0; slph ^= 1u; }
           }
         }
       }

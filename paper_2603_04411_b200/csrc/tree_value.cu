@@ -1,13 +1,15 @@
 // Weighted values of drafted trees on the 5th-generation tensor cores.
 //
 // As in a decode pass (vacc_tc.cu) the weighted sum is taken in spectral space:
-//   acc[j][c] = sum over the split's tokens t of X^_V[t][j] p[t][c],   p = exp(s - max),   l[c] = sum of p[t][c]
+//   acc[j][c] = sum over the split's tokens t of X^_V[t][j] p[t][c],   p = exp(s - top[c]),   l[c] = sum of p[t][c]
 // for 64 columns c = (KV head, node, head of the group) per CTA.  Two panels of a V tile are the A operand (M = 128 spectral columns, as TMA
 // lands them: MN-major), the weights of 16 tokens and 64 columns the B operand.  Weights go in as two parts of the cache type, both into one
 // accumulator (64 columns of tensor memory per pair of panels: 512 for d_kv = 1024), so that a CTA serves twice the columns of a decode CTA
 // and the panels are read from L2 half as often.
 // The scores of a tile are read a tile ahead into registers (thread = one column, 32 tokens): 32 lanes read 32 columns of a token, a whole
 // line, and no room in shared memory goes to them.
+// What a column's weights are relative to, top[c], is the largest score so far, moved only when it would grow by more than 2^8 (f16 holds 2^15):
+// the sums in tensor memory are rescaled seldom, by the weight warps themselves.  The merge brings the splits' parts together.
 // Tiles that are at most half full, and the nodes' tile, are read by the boxes of sixteen rows that hold tokens.
 //
 // Warp roles (320 threads, one CTA per SM): 0 TMA producer of V panels, 1 MMA issuer (owns the TMEM allocation), 2-9 weights, then the read-out.
@@ -27,7 +29,7 @@ constexpr int TV_STAGES = 4;
 constexpr uint32_t TV_PANEL = 16384, TV_STAGE = 2 * TV_PANEL;
 constexpr uint32_t TV_ZERO = 2048;                             // 16 token rows of zeros: the missing partner of a lone panel
 constexpr uint32_t TV_P_PART = TV_N * 128, TV_P_HALF = 2 * TV_P_PART, TV_P_BUF = 2 * TV_P_HALF;      // [2 halves of 64 tokens][high, low][64 columns][64 tokens]
-constexpr uint32_t TV_SMEM = TV_STAGES * TV_STAGE + TV_ZERO + 2 * TV_P_BUF + TV_META * 16 + TV_PTHREADS * 4 + 256 + 1024;
+constexpr uint32_t TV_SMEM = TV_STAGES * TV_STAGE + TV_ZERO + 2 * TV_P_BUF + TV_META * 16 + 2 * TV_PTHREADS * 4 + TV_N * 4 + 256 + 1024;
 static_assert(TV_SMEM > CHAIN_TMEM_SMEM && TV_SMEM <= 232448, "no other CTA with tensor memory beside this one");
 constexpr int TV_OUT = 32;                                     // columns of the partial result on their way out at a time
 static_assert(TV_OUT * TWKV_MAX_CLASSES * PANEL * 4 <= (int)(TV_STAGES * TV_STAGE), "the partial sums leave through the ring's memory");
@@ -48,7 +50,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int d_kv = v.d_kv;
   const int req = blockIdx.x / a.n_splits, split = blockIdx.x - req * a.n_splits, c0 = blockIdx.y * TV_N;
-  // shared memory: ring | zero block | weights [2 buffers] | descriptors | row sums | barriers
+  // shared memory: ring | zero block | weights [2 buffers] | descriptors | row sums | maxima, factors | barriers
   const uint32_t s0 = smem_addr(smem_raw);
   const uint32_t pad = (1024u - (s0 & 1023u)) & 1023u;          // operand tiles need 1024-byte alignment for the swizzle
   unsigned char* base_ptr = smem_raw + pad;
@@ -56,7 +58,8 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   unsigned char* sP_ptr = base_ptr + TV_STAGES * TV_STAGE + TV_ZERO;
   int4* s_meta = reinterpret_cast<int4*>(sP_ptr + 2 * TV_P_BUF);
   float* s_l = reinterpret_cast<float*>(s_meta + TV_META);
-  unsigned char* tail = reinterpret_cast<unsigned char*>(s_l + TV_PTHREADS);
+  float *s_max = s_l + TV_PTHREADS, *s_f = s_max + TV_PTHREADS;   // a tile's maxima per thread; factors of the columns' sums
+  unsigned char* tail = reinterpret_cast<unsigned char*>(s_f + TV_N);
   const uint32_t bars = smem_addr(tail);
   const uint32_t full = bars, empty = full + 8 * TV_STAGES, p_full = empty + 8 * TV_STAGES, p_empty = p_full + 16, acc_done = p_empty + 16;
   uint32_t* s_tmem_base = reinterpret_cast<uint32_t*>(tail + 8 * (2 * TV_STAGES + 5));
@@ -95,13 +98,9 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   uint64_t l_sum2 = 0;                                          // weight threads: two sums of this thread's weights
   const int pt = tid - 64, pc = pt & (TV_N - 1), tg0 = pt >> 6; // weight threads: column; token groups tg0, tg0 + 4, ...
   const bool in = c0 + pc < a.C;
-  uint64_t nm2 = 0;                                             // minus the column's maximum, in powers of two
-  const uint64_t log2e2 = tv_pack(TV_LOG2E, TV_LOG2E);
-  if (warp >= 2) {
-    const float m = in ? dec_ordered(a.seqmax[(size_t)req * a.C + c0 + pc]) : 0.f;
-    const float m_c = m == -INFINITY ? 0.f : m;                 // (a node that sees nothing has no maximum: weights stay 0)
-    nm2 = tv_pack(-m_c * TV_LOG2E, -m_c * TV_LOG2E);
-  }
+  const float scale = (v.sm_scale == 0.f ? 1.f : fabsf(v.sm_scale)) * TV_LOG2E;      // scores come without their scale; weights are powers of two
+  const uint64_t scale2 = tv_pack(scale, scale);
+  float top = -INFINITY;                                        // weight threads: what the column's weights are relative to, times scale
 
   for (int k0 = 0; k0 < n_mine; k0 += TV_META) {
     const int cn = min(TV_META, n_mine - k0);
@@ -199,13 +198,55 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
       };
       float cur[32], nxt[32];
       read(0, cur);
-      for (int i = 0; i < cn && ok; ++i) {
+      for (int i = 0; i < cn; ++i) {
         const int k = k0 + i;
         const int4 m = s_meta[i];
-        max_cls = max(max_cls, m.y);
         read(i + 1, nxt);
+        // the tile's maximum of the column, from the four threads that share it
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int u = 0; u < 32; u += 4)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], cur[u + e]);
+        s_max[pt] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        // a wait that ran out in one warp ends the loop in all of them, here: none is left at a barrier
+        if (!(ok = named_bar_and(1, TV_PTHREADS, ok))) break;
+        const float most = fmaxf(fmaxf(s_max[pc], s_max[pc + 64]), fmaxf(s_max[pc + 128], s_max[pc + 192])) * scale;
+        const bool grow = most > top + 8.f;                       // also the first finite maximum
+        const float next = grow ? most : top, f = next == top ? 1.f : tv_ex2(top - next);      // 0 where there was none yet
+        top = next;
+        if (tg0 == 0) s_f[pc] = f;
+        float la, lb;
+        tv_unpack(l_sum2, la, lb);
+        l_sum2 = tv_pack(la * f, lb * f);
+        if (!named_bar_and(1, TV_PTHREADS, !grow) && k > 0) {
+          // seldom: what has been summed takes the factors, once the products so far have retired (those of this tile wait for its weights)
+          ok = __all_sync(0xffffffffu, mbar_wait(p_empty + 8 * ((uint32_t)(k - 1) & 1u), ((uint32_t)(k - 1) >> 1) & 1u, abort_flag));
+          fence_after_sync();
+          const int pairs = ok ? (max_cls + 1) >> 1 : 0;
+#pragma unroll 1
+          for (int pair = (warp - 2) >> 2; pair < pairs; pair += 2) {
+            const uint32_t at = tmem_base + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(pair * TV_N);
+#pragma unroll 1
+            for (int c = 0; c < TV_N; c += 8) {
+              uint32_t o[8];
+              tmem_ld8(at + c, o);
+              tmem_ld_wait();
+#pragma unroll
+              for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * s_f[c + e]);
+              tmem_st8(at + c, o);
+            }
+          }
+          tmem_st_wait();
+          fence_before_sync();
+          if (!(ok = named_bar_and(1, TV_PTHREADS, ok))) break;   // the factors have been read, the sums are whole
+        }
+        max_cls = max(max_cls, m.y);
         const uint32_t buf = (uint32_t)k & 1u;
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(p_empty + 8 * buf, (((uint32_t)k >> 1) & 1u) ^ 1u, abort_flag)))) break;
+        ok = __all_sync(0xffffffffu, mbar_wait(p_empty + 8 * buf, (((uint32_t)k >> 1) & 1u) ^ 1u, abort_flag));
+        if (!ok) continue;
+        const float ref = top == -INFINITY ? 0.f : top;           // (a node that sees nothing so far has no maximum: weights stay 0)
+        const uint64_t nm2 = tv_pack(-ref, -ref);
         unsigned char* pb = sP_ptr + buf * TV_P_BUF;
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
@@ -215,7 +256,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
 #pragma unroll
           for (int u = 0; u < 8; u += 2) {
             float x0, x1;
-            tv_unpack(tv_fma2(tv_pack(cur[it * 8 + u], cur[it * 8 + u + 1]), log2e2, nm2), x0, x1);
+            tv_unpack(tv_fma2(tv_pack(cur[it * 8 + u], cur[it * 8 + u + 1]), scale2, nm2), x0, x1);
             const uint64_t p = tv_pack(tv_ex2(x0), tv_ex2(x1));
             l_sum2 = tv_add2(l_sum2, p);
             split_pair_16<BF16>(p, hi[u >> 1], lo[u >> 1]);
@@ -246,6 +287,8 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     tv_unpack(l_sum2, x, y);
     s_l[pt] = x + y;
     bool ready = ok;
+    if (n_mine > 0) named_bar_sync(1, TV_PTHREADS);             // the last tile's maxima have been read
+    if (tg0 == 0) s_max[pc] = top;
     if (ready && n_mine > 0) ready = __all_sync(0xffffffffu, mbar_wait(acc_done, 0u, abort_flag));
     fence_after_sync();
     const int quad = warp & 3;                                  // the TMEM lanes this warp may read
@@ -292,7 +335,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   if (warp == 1) tmem_dealloc(tmem_base, tmem_cols);
   if (tid < TV_N) {
     const int r = part_row(c0 + tid);
-    if (r >= 0) a.part_l[r] = (s_l[tid] + s_l[tid + 64]) + (s_l[tid + 128] + s_l[tid + 192]);
+    if (r >= 0) a.part_ml[r] = make_float2(s_max[tid], (s_l[tid] + s_l[tid + 64]) + (s_l[tid + 128] + s_l[tid + 192]));
   }
   if (tid == 0 && *abort_flag) set_status(v, TWKV_ERR_TIMEOUT);
 }
