@@ -843,7 +843,7 @@ static size_t tree_layout(const twkv_cache* c, TreeCall& a, unsigned char* base)
     return p;
   };
   // (room for n_splits of a request each; counted so that more requests never ask for less)
-  const size_t n = a.n_req, tiles = (size_t)v.TPS + 1, fill = std::min(n * TREE_MAX_SPLITS, (size_t)c->sm_count / ((a.C + 63) / 64));
+  const size_t n = a.n_req, tiles = (size_t)v.TPS + 1, fill = std::min(n * TREE_MAX_SPLITS, (size_t)c->sm_count / ((a.C + TILE - 1) / TILE));
   const size_t parts = std::max(n, fill) * a.T * v.Hq;
   a.nk = take(n * v.NC * TREE_PANEL_ROWS * PANEL * 2);
   a.nv = take(n * v.NC * TREE_PANEL_ROWS * PANEL * 2);
@@ -856,7 +856,8 @@ static size_t tree_layout(const twkv_cache* c, TreeCall& a, unsigned char* base)
   a.vcut = (int*)take(n * (a.n_splits + 1) * sizeof(int));
   a.cta_start = (int*)take((MAX_PLAN_CTAS + 1) * sizeof(int));
   a.parts = (int*)take(sizeof(int));
-  a.part_ml = (float2*)take(parts * sizeof(float2));
+  a.part_ml = (float4*)take(parts * sizeof(float4));
+  a.part_cls = (int*)take(std::max(n, fill) * sizeof(int));
   a.part_acc = (float*)take(parts * v.d_kv * sizeof(float));
   a.scores = (float*)take(n * tiles * TILE * a.C * sizeof(float));
   return at;
@@ -869,7 +870,7 @@ static TreeCall tree_shape(const twkv_cache* c, int n_req, int max_nodes) {
   a.n_req = n_req; a.T = max_nodes;
   a.R = max_nodes * v.rep; a.Rs = a.R > 4 ? (a.R + 7) & ~7 : 4; a.Rp = (a.R + 15) & ~15; a.C = v.Hkv * a.Rs;
   a.entries = (v.TPS + 4) & ~1;
-  a.n_splits = std::max(1, std::min(TREE_MAX_SPLITS, c->sm_count / (n_req * ((a.C + 63) / 64))));
+  a.n_splits = std::max(1, std::min(TREE_MAX_SPLITS, c->sm_count / (n_req * ((a.C + TILE - 1) / TILE))));
   return a;
 }
 

@@ -10,6 +10,8 @@
 
 namespace twkv {
 
+constexpr int TREE_RANGE = 6;                    // panels whose sums a CTA of the value kernel keeps
+static_assert((TWKV_MAX_CLASSES + TREE_RANGE - 1) / TREE_RANGE <= 3, "three ranges beside the sum of the weights");
 constexpr int TREE_MAX_SPLITS = 64;              // of a request's V tiles
 constexpr int TREE_PANEL_ROWS = 64;              // rows of a panel of the nodes' tiles
 static_assert(TWKV_TREE_MAX_NODES <= TREE_PANEL_ROWS && TWKV_TREE_MAX_NODES <= 64, "a node is a bit of a 64-bit word, and a row of a panel");
@@ -44,7 +46,8 @@ struct TreeCall {
   int* vcut;            // [n_req][n_splits + 1]
   int *cta_start, *parts;     // [pieces + 1] first item part of a piece; parts of an item
   float* part_acc;      // [n_req][T][n_splits][Hq][d_kv]
-  float2* part_ml;      // [n_req][T][n_splits][Hq] maximum of the split (powers of two), sum of its weights
+  float4* part_ml;      // [n_req][T][n_splits][Hq] what the split's weights are relative to (powers of two) in each range of panels, their sum
+  int* part_cls;        // [n_req][n_splits] widest class of the split's tiles, 0: none
 };
 
 // The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the

@@ -69,33 +69,40 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     if (!row_at(r, req, t)) continue;
     const int used = a.info[req].w;                             // splits that hold something come first
     const size_t row = (size_t)(req * a.T + t) * a.n_splits * v.Hq + g * rep + r % rep;
-    const int* cut = a.vcut + (size_t)req * (a.n_splits + 1);
-    // lane = split, or two: their weights relative to the largest maximum, and the sum of all weights
-    float top[2], l[2], w[2];
+    // lane = split, or two: what their weights are relative to and their sums; the largest of the first, the sum of all weights
+    float top[2], l[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float2 ml = lane + 32 * h < used ? a.part_ml[row + (size_t)(lane + 32 * h) * v.Hq] : make_float2(-INFINITY, 0.f);
-      top[h] = ml.x; l[h] = ml.y;
+      const float4 ml = lane + 32 * h < used ? a.part_ml[row + (size_t)(lane + 32 * h) * v.Hq] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+      top[h] = ml.x; l[h] = ml.w;
     }
     float most = fmaxf(top[0], top[1]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float sum = 0.f;                                             // (one that is not a number stays one)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) w[h] = top[h] == -INFINITY ? 0.f : tm_ex2(top[h] - most);
-    float sum = l[0] * w[0] + l[1] * w[1];                       // (a sum that is not a number stays one)
+    for (int h = 0; h < 2; ++h) sum += l[h] * (top[h] == -INFINITY ? 0.f : tm_ex2(top[h] - most));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float il = sum == 0.f ? 0.f : 1.f / sum;               // 0: no token seen
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    // the components of a range of panels have a reference of their own; behind the split's widest class there are none
+    const int comp = j0 + lane * 4, range = comp / (TREE_RANGE * PANEL);
     const float4* p = reinterpret_cast<const float4*>(a.part_acc + row * v.d_kv + j0) + lane;
+    const float* refs = reinterpret_cast<const float*>(a.part_ml + row) + range;
+    const int* cls = a.part_cls + (size_t)req * a.n_splits;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int s0 = 0; s0 < used; s0 += 8) {
       float4 y[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        y[k] = lane * 4 < jn && s0 + k < used && cut[s0 + k + 1] > cut[s0 + k] ? p[(size_t)(s0 + k) * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
+      float w[8];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float ws = __shfl_sync(0xffffffffu, s0 < 32 ? w[0] : w[1], (s0 + k) & 31);
+        const bool in = lane * 4 < jn && s0 + k < used && comp < cls[s0 + k] * PANEL;
+        y[k] = in ? p[(size_t)(s0 + k) * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
+        w[k] = in ? refs[(size_t)(s0 + k) * v.Hq * 4] : -INFINITY;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float ws = w[k] == -INFINITY ? 0.f : tm_ex2(w[k] - most);
         x.x += y[k].x * ws; x.y += y[k].y * ws; x.z += y[k].z * ws; x.w += y[k].w * ws;
       }
     }
@@ -106,8 +113,8 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
       split_pair_16<BF16>(w, hi[0], lo[0]);
       asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.z * il), "f"(x.w * il));
       split_pair_16<BF16>(w, hi[1], lo[1]);
-      const int comp = lane * 4;
-      unsigned char* d = smem + (comp >> 6) * TM_PANEL + r * 128 + ((((comp >> 3) & 7) ^ (r & 7)) << 4) + (comp & 7) * 2;
+      const int e = lane * 4;
+      unsigned char* d = smem + (e >> 6) * TM_PANEL + r * 128 + ((((e >> 3) & 7) ^ (r & 7)) << 4) + (e & 7) * 2;
       *reinterpret_cast<uint2*>(d) = make_uint2(hi[0], hi[1]);
       *reinterpret_cast<uint2*>(d + 2 * TM_PANEL) = make_uint2(lo[0], lo[1]);
     }

@@ -20,9 +20,11 @@
 
 namespace twkv {
 
-// Estimated cycles of an item of the score kernel.
+// Estimated cycles of an item of the score kernel: per KV head and pass a part for rotation and score products, which grow with the query rows, beyond
+// 64 with the stores of the scores; and a part per panel.  Fitted to lists of one class (16 to 512 query rows, 1 to 16 panels).  Only the ratios matter.
 __device__ __forceinline__ unsigned tree_cost(const DevView& v, const TreeCall& a, int cls) {
-  return (unsigned)v.Hkv * (1500u + 250u * (unsigned)cls + 300u * (unsigned)((a.R + 63) / 64));
+  const unsigned rows = 14u * (unsigned)min(a.R, 64) + 28u * (unsigned)max(a.R - 64, 0), passes = cls > 8 ? 2u : 1u;
+  return (unsigned)v.Hkv * (passes * (1500u + rows) + 300u * (unsigned)cls);
 }
 
 // Refuses a request whose sequence an earlier one names, or into whose rows an earlier one reaches: those are not its to write (the
@@ -275,7 +277,8 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
       m = make_int4(i * (v.TPS + 1) + nv, r.w >> 8, r.y, -1);
     }
     meta[k] = m;
-    return TILE / 32 * vtile_boxes(m.z) * m.y + 64;
+    // in panels' products: a tile's weights take as long as those of four panels; wide tiles are taken in ranges of six, by CTAs of their own
+    return vtile_boxes(m.z) * max(min(m.y, TREE_RANGE), 4) + 4;
   };
   int total = 0;
   for (int k0 = 0; k0 < n; k0 += 1024) {

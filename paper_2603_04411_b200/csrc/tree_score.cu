@@ -17,7 +17,8 @@
 //   warps 4-11  rotation and high / low split (thread = one token row x half of the RoPE frequencies)
 //   warps 12-15 scores out: masked (nodes), stored in the order of the V tiles (thread = one token row)
 // Scores are stored without their scale, which the value kernel's exponents carry (a negative scale is in the queries).
-// A class wider than eight panels runs as two passes over its panels, the second adding to the scores the first one stored.
+// A class wider than eight panels runs as two passes over its panels, the second adding to the scores the first one stored (one addition
+// per score, in memory: its order cannot vary).
 // All waits are bounded (tc_util.cuh); a wait that runs out ends the kernel with TWKV_ERR_TIMEOUT.
 #include "twkv_dev.h"
 #include "tc_util.cuh"
@@ -451,24 +452,19 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(s_empty_even + 8 * slot);
               }
-              if (ps > 0 && live) {                                // what this thread stored of the first pass
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                  if (32 * ch + 8 * c < cols) {
-                    const float4* p = reinterpret_cast<const float4*>(dst + 32 * ch + 8 * c);
-                    const float4 y = p[0], z = a.Rs >= 8 ? p[1] : make_float4(0.f, 0.f, 0.f, 0.f);
-                    const float o[8] = {y.x, y.y, y.z, y.w, z.x, z.y, z.z, z.w};
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) x[8 * c + e] = __float_as_uint(__uint_as_float(x[8 * c + e]) + o[e]);
-                  }
-              }
               if (node) {                                          // a node is seen by the queries whose masks hold its bit
                 const unsigned bits = (unsigned)(seers >> ((sub * TS_QCOLS + 32 * ch) >> rep_shift));       // (32 columns are at most 32 nodes)
 #pragma unroll
                 for (int c = 0; c < 32; ++c)
                   if (!((bits >> (c >> rep_shift)) & 1u)) x[c] = 0xff800000u;
               }
-              if (live) {
+              if (live && ps > 0) {                                // onto what this thread stored of the first pass
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                  if (32 * ch + 4 * c < cols)
+                    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(__cvta_generic_to_global(dst + 32 * ch + 4 * c)), "f"(__uint_as_float(x[4 * c])),
+                                 "f"(__uint_as_float(x[4 * c + 1])), "f"(__uint_as_float(x[4 * c + 2])), "f"(__uint_as_float(x[4 * c + 3])) : "memory");
+              } else if (live) {
                 if (a.Rs >= 8) {
 #pragma unroll
                   for (int c = 0; c < 4; ++c)
