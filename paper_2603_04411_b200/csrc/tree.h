@@ -34,6 +34,7 @@ struct TreeCall {
   int n_splits;
   int entries;          // room of a request in the K list
   int q_box;            // rows of qop that a CTA takes at a time
+  int v_box;            // score columns that a CTA of the value kernel takes, at most 128
   // workspace
   unsigned short* qop;  // [n_req][Hkv][Rp][128] f16 queries in the order of the score contraction
   unsigned char *nk, *nv;     // [n_req][NC][64 rows][64] panels of the nodes' keys and values
@@ -51,8 +52,9 @@ struct TreeCall {
 };
 
 // The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the
-// queries, U_V^-1 (an eighth of its rows, 64 columns).
-struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q, uv; };
+// queries, U_V^-1 (an eighth of its rows, 64 columns), the
+// scores (a tile's rows or sixteen of them, v_box columns).
+struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q, uv, scores, score_boxes; };
 
 // Rows of tree i; false where the offsets do not describe at most max_nodes rows of n_rows.
 __device__ __forceinline__ bool tree_rows(const int* offsets, int i, int n_rows, int max_nodes, int* first, int* n) {

@@ -19,8 +19,9 @@ using namespace tc;
 constexpr int TM_THREADS = 256, TM_CL = 8;
 constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 components] of one part
 constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // high and low parts of up to 128 components; their rows of U_V^-1, 128 columns
-constexpr uint32_t TM_SMEM = TM_A + TM_B + 64;
-static_assert(TREE_MAX_SPLITS <= 64, "two splits per lane");
+constexpr int TM_FEW = 4;                                     // splits whose weights are looked up once per row
+constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16 + TM_FEW * 2 * 4 + TM_FEW) + 64;
+static_assert(2 * TM_SMEM <= 228 * 1024 - 2 * 1024, "two CTAs per SM");
 static_assert(TM_CL * TILE * (HEAD_DIM / TM_CL) * 4 <= TM_A, "the partial products arrive where the A operand was");
 
 __device__ __forceinline__ float tm_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
@@ -29,8 +30,12 @@ template <bool BF16>
 __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
-  const uint32_t b_full = sB + TM_B, done = b_full + 8;
-  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(smem + TM_A + TM_B + 16);
+  float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE, *s_w = s_inv + TILE;      // per row
+  int4* s_row = reinterpret_cast<int4*>(s_w + TILE * TM_FEW * 2);                     // first part, splits, request, row of the outputs; -1: none
+  unsigned char* s_cls = reinterpret_cast<unsigned char*>(s_row + TILE);
+  unsigned char* tail = s_cls + TILE * TM_FEW;
+  const uint32_t b_full = smem_addr(tail), done = b_full + 8;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(tail + 16);
   volatile int* abort_flag = reinterpret_cast<int*>(s_tmem + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int c = (int)cluster_cta_rank(), g = blockIdx.y, rep = v.rep, jn = v.d_kv / TM_CL, j0 = c * jn;      // jn: a multiple of 16, at most 128
@@ -56,67 +61,118 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   }
   __syncwarp();
 
-  // rows: a warp each, its lanes four components; row (slot, h), slot = request * T + node
-  auto row_at = [&](int r, int& req, int& t) -> bool {
-    const int slot = slot0 + r / rep;
-    req = slot / a.T;
-    t = slot - req * a.T;
-    return slot < n_slots && t < a.info[req].y;
+  // A thread per row (slot, h), slot = request * T + node: where its parts are, the largest reference of its splits, one over the sum of all weights;
+  // and what the parts of the first splits are worth.  The components of a range of panels have a reference of their own; behind a split's
+  // widest class there are none.  Looked up here once, so that the reads below depend on shared memory only.
+  const int range0 = j0 / (TREE_RANGE * PANEL);               // of the CTA's first components; a later one may lie in the next range
+  if (tid < TILE) {
+    const int slot = slot0 + tid / rep, req = slot / a.T, t = slot - req * a.T;
+    int row = -1, used = 0;
+    float most = -INFINITY, sum = 0.f;
+    int4 info = make_int4(0, 0, 0, 0);
+    if (slot < n_slots) info = a.info[req];
+    if (slot < n_slots && t < info.y) {
+      used = info.w;                                            // splits that hold something come first
+      row = slot * a.n_splits * v.Hq + g * rep + tid % rep;
+      const float4* ml = a.part_ml + row;
+      for (int s0 = 0; s0 < used; s0 += 4) {
+        float4 y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = s0 + k < used ? ml[(size_t)(s0 + k) * v.Hq] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        const float m = fmaxf(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), most);
+        sum *= most == -INFINITY ? 0.f : tm_ex2(most - m);      // (one that is not a number stays one)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum += y[k].w * (y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m));
+        most = m;
+        if (used <= TM_FEW) {
+#pragma unroll
+          for (int k = 0; k < TM_FEW; ++k) {
+            const float r0 = range0 == 0 ? y[k].x : range0 == 1 ? y[k].y : y[k].z, r1 = range0 == 0 ? y[k].y : y[k].z;
+            s_cls[tid * TM_FEW + k] = k < used ? (unsigned char)a.part_cls[req * a.n_splits + k] : 0;
+            s_w[(tid * TM_FEW + k) * 2] = r0 == -INFINITY ? 0.f : tm_ex2(r0 - m);
+            s_w[(tid * TM_FEW + k) * 2 + 1] = r1 == -INFINITY ? 0.f : tm_ex2(r1 - m);
+          }
+        }
+      }
+    }
+    s_row[tid] = make_int4(row, used, req, slot < n_slots && t < info.y ? info.x + t : -1);
+    s_most[tid] = most;
+    s_inv[tid] = sum == 0.f ? 0.f : 1.f / sum;                  // 0: no token seen
+  }
+  __syncthreads();
+  // Sums: a warp takes rows warp, warp + 8, ..., its lanes four components.  Eight reads on their way: of as many rows where a row has few splits, of
+  // eight splits otherwise.  (16384 rows of one split one after the other took 204 us.)
+  const int comp = j0 + lane * 4, range = comp / (TREE_RANGE * PANEL);
+  const bool mine = lane * 4 < jn;
+  auto put = [&](int r, float4 x) {                             // a row's normalised components as the A operand
+    if (!mine) return;
+    const float il = s_inv[r];
+    uint32_t hi[2], lo[2];
+    uint64_t w;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.x * il), "f"(x.y * il));
+    split_pair_16<BF16>(w, hi[0], lo[0]);
+    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.z * il), "f"(x.w * il));
+    split_pair_16<BF16>(w, hi[1], lo[1]);
+    const int e = lane * 4;
+    unsigned char* d = smem + (e >> 6) * TM_PANEL + r * 128 + ((((e >> 3) & 7) ^ (r & 7)) << 4) + (e & 7) * 2;
+    *reinterpret_cast<uint2*>(d) = make_uint2(hi[0], hi[1]);
+    *reinterpret_cast<uint2*>(d + 2 * TM_PANEL) = make_uint2(lo[0], lo[1]);
   };
-  const size_t stride = (size_t)v.Hq * v.d_kv / 4;              // float4 from split to split
-  for (int r = warp; r < TILE; r += TM_THREADS / 32) {
-    int req, t;
-    if (!row_at(r, req, t)) continue;
-    const int used = a.info[req].w;                             // splits that hold something come first
-    const size_t row = (size_t)(req * a.T + t) * a.n_splits * v.Hq + g * rep + r % rep;
-    // lane = split, or two: what their weights are relative to and their sums; the largest of the first, the sum of all weights
-    float top[2], l[2];
+  const float* const acc = a.part_acc + comp;
+  if (a.n_splits <= TM_FEW) {
+#pragma unroll 1
+    for (int b = 0; b < TILE / 8; b += 8) {
+      float4 x[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float4 ml = lane + 32 * h < used ? a.part_ml[row + (size_t)(lane + 32 * h) * v.Hq] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
-      top[h] = ml.x; l[h] = ml.w;
-    }
-    float most = fmaxf(top[0], top[1]);
+      for (int k = 0; k < 8; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+      for (int s = 0; s < a.n_splits; ++s) {
+        float4 y[8];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-    float sum = 0.f;                                             // (one that is not a number stays one)
+        for (int k = 0; k < 8; ++k) {
+          const int r = warp + 8 * (b + k);
+          const int4 q = s_row[r];
+          const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
+          y[k] = in ? *reinterpret_cast<const float4*>(acc + (size_t)(q.x + s * v.Hq) * v.d_kv) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) sum += l[h] * (top[h] == -INFINITY ? 0.f : tm_ex2(top[h] - most));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const float il = sum == 0.f ? 0.f : 1.f / sum;               // 0: no token seen
-    // the components of a range of panels have a reference of their own; behind the split's widest class there are none
-    const int comp = j0 + lane * 4, range = comp / (TREE_RANGE * PANEL);
-    const float4* p = reinterpret_cast<const float4*>(a.part_acc + row * v.d_kv + j0) + lane;
-    const float* refs = reinterpret_cast<const float*>(a.part_ml + row) + range;
-    const int* cls = a.part_cls + (size_t)req * a.n_splits;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s0 = 0; s0 < used; s0 += 8) {
-      float4 y[8];
-      float w[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const bool in = lane * 4 < jn && s0 + k < used && comp < cls[s0 + k] * PANEL;
-        y[k] = in ? p[(size_t)(s0 + k) * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
-        w[k] = in ? refs[(size_t)(s0 + k) * v.Hq * 4] : -INFINITY;
+        for (int k = 0; k < 8; ++k) {
+          const int r = warp + 8 * (b + k);
+          const int4 q = s_row[r];
+          const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
+          const float w = in ? s_w[(r * TM_FEW + s) * 2 + range - range0] : 0.f;
+          x[k].x += y[k].x * w; x[k].y += y[k].y * w; x[k].z += y[k].z * w; x[k].w += y[k].w * w;
+        }
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float ws = w[k] == -INFINITY ? 0.f : tm_ex2(w[k] - most);
-        x.x += y[k].x * ws; x.y += y[k].y * ws; x.z += y[k].z * ws; x.w += y[k].w * ws;
-      }
+      for (int k = 0; k < 8; ++k) put(warp + 8 * (b + k), x[k]);
     }
-    if (lane * 4 < jn) {
-      uint32_t hi[2], lo[2];
-      uint64_t w;
-      asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.x * il), "f"(x.y * il));
-      split_pair_16<BF16>(w, hi[0], lo[0]);
-      asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.z * il), "f"(x.w * il));
-      split_pair_16<BF16>(w, hi[1], lo[1]);
-      const int e = lane * 4;
-      unsigned char* d = smem + (e >> 6) * TM_PANEL + r * 128 + ((((e >> 3) & 7) ^ (r & 7)) << 4) + (e & 7) * 2;
-      *reinterpret_cast<uint2*>(d) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2*>(d + 2 * TM_PANEL) = make_uint2(lo[0], lo[1]);
+  } else {
+#pragma unroll 1
+    for (int r = warp; r < TILE; r += TM_THREADS / 32) {
+      const int4 q = s_row[r];
+      if (q.x < 0) continue;
+      const int* cls = a.part_cls + q.z * a.n_splits;
+      const float* refs = reinterpret_cast<const float*>(a.part_ml + q.x) + range;
+      const float most = s_most[r];
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+      for (int s0 = 0; s0 < q.y; s0 += 8) {
+        float4 y[8];
+        float ref[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const bool in = mine && s0 + k < q.y && comp < cls[s0 + k] * PANEL;
+          y[k] = in ? *reinterpret_cast<const float4*>(acc + (size_t)(q.x + (s0 + k) * v.Hq) * v.d_kv) : make_float4(0.f, 0.f, 0.f, 0.f);
+          ref[k] = in ? refs[(size_t)(s0 + k) * v.Hq * 4] : -INFINITY;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float w = ref[k] == -INFINITY ? 0.f : tm_ex2(ref[k] - most);
+          x.x += y[k].x * w; x.y += y[k].y * w; x.z += y[k].z * w; x.w += y[k].w * w;
+        }
+      }
+      put(r, x);
     }
   }
   fence_proxy_async_smem();
@@ -164,8 +220,8 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   if (warp == 1) tmem_dealloc(tmem, 128);
   {
     const int r = tid >> 1, e0 = (tid & 1) * 8;
-    int req, t;
-    if (row_at(r, req, t)) {
+    const int4 q = s_row[r];
+    if (q.w >= 0) {
       const float* in = reinterpret_cast<const float*>(smem) + r * 16 + e0;
       float o[8];
 #pragma unroll
@@ -175,12 +231,11 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
         const float4 x = *reinterpret_cast<const float4*>(in + k * TILE * 16), y = *reinterpret_cast<const float4*>(in + k * TILE * 16 + 4);
         o[0] += x.x; o[1] += x.y; o[2] += x.z; o[3] += x.w; o[4] += y.x; o[5] += y.y; o[6] += y.z; o[7] += y.w;
       }
-      const int4 info = a.info[req];
-      if (info.z >= 0 && (a.masks[info.x + t] & a.bad[req])) {  // sees a node whose value is not finite
+      if (q.y > 0 && (a.masks[q.w] & a.bad[q.z])) {  // sees a node whose value is not finite
 #pragma unroll
         for (int e = 0; e < 8; ++e) o[e] = __int_as_float(0x7fffffff);
       }
-      const size_t at = ((size_t)(info.x + t) * v.Hq + g * rep + r % rep) * HEAD_DIM + c * 16 + e0;
+      const size_t at = ((size_t)q.w * v.Hq + g * rep + r % rep) * HEAD_DIM + c * 16 + e0;
       if (v.out_dtype == TWKV_F32) {
         float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at);
         d[0] = make_float4(o[0], o[1], o[2], o[3]);

@@ -8,12 +8,13 @@
 // work took 85 cycles for its operands instead of 32: 12200 cycles per tile of sixteen panels and 64 columns.)
 // Tensor memory holds the weights of one tile (128 columns: 64 of high parts, 64 of low ones) and three accumulators of 128 columns: six panels.  A
 // CTA therefore takes a range of six panels (blockIdx.z); the wider ranges, which only wide tiles reach, form those tiles' weights again.
-// Scores are read a tile ahead into registers: lanes are consecutive columns of a token, a whole line.  What a row's weights are relative to, top[c],
+// A tile's scores come by TMA while the tile before is worked on (read from memory by the lanes themselves, whose registers hold one tile, their
+// latency bound the kernel: 5600 cycles per narrow tile).  What a row's weights are relative to, top[c],
 // is its largest score so far, moved only when it would grow by more than 2^8 (f16 holds 2^15): the accumulators are rescaled seldom, by the
 // warps that own their lanes.  The merge brings the splits' parts together.
 // Tiles that are at most half full, and the nodes' tile, are read by the boxes of sixteen rows that hold tokens.
 //
-// Warp roles (640 threads, one CTA per SM): 0 TMA producer of V panels, 1 MMA issuer (owns the TMEM allocation), 2 and 3 idle, 4-19 weights
+// Warp roles (640 threads, one CTA per SM): 0 TMA producer of V panels, 1 MMA issuer (owns the TMEM allocation), 2 TMA producer of scores, 4-19 weights
 // (quarter = warp % 4 of the rows, part (warp - 4) / 4 of the tile's tokens), then the read-out.
 // All waits are bounded (tc_util.cuh); a wait that runs out ends the kernel with TWKV_ERR_TIMEOUT.
 #include "twkv_dev.h"
@@ -26,10 +27,11 @@ using namespace tc;
 constexpr int TV_THREADS = 640;
 constexpr int TV_REGS_LIGHT = 64, TV_REGS_WEIGHTS = 104;       // 128 x 64 + 512 x 104 = 61440 = 640 x 96
 constexpr int TV_META = 256;                                   // tiles whose descriptors are staged in shared memory at a time
-constexpr int TV_STAGES = 6;
+constexpr int TV_STAGES = 4;
 constexpr uint32_t TV_PANEL = 16384, TV_STAGE = 2 * TV_PANEL;
 constexpr uint32_t TV_COL_P = 384;                             // behind three accumulators
-constexpr uint32_t TV_SMEM = TV_STAGES * TV_STAGE + TV_META * 16 + 2 * 4 * TILE * 4 + 256;
+constexpr uint32_t TV_SCORES = TILE * TILE * 4;                 // a tile's scores with 128 query rows
+constexpr uint32_t TV_SMEM = TV_STAGES * TV_STAGE + TV_SCORES + TV_META * 16 + 2 * 4 * TILE * 4 + 256;
 static_assert(TV_SMEM > CHAIN_TMEM_SMEM && TV_SMEM <= 232448, "no other CTA with tensor memory beside this one");
 static_assert(TREE_RANGE == 6, "three accumulators of two panels");
 static_assert(2 * TREE_PANEL_ROWS <= TILE, "the nodes' tile always comes in boxes");
@@ -44,26 +46,30 @@ __device__ __forceinline__ float tv_ex2(float x) { float r; asm("ex2.approx.ftz.
 template <bool BF16>
 __global__ void __launch_bounds__(TV_THREADS, 1)
 tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_constant__ CUtensorMap map_boxes, const __grid_constant__ CUtensorMap map_nodes,
-                  DevView v, TreeCall a) {
+                  const __grid_constant__ CUtensorMap map_scores, const __grid_constant__ CUtensorMap map_score_boxes, DevView v, TreeCall a) {
   chain_start();
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int req = blockIdx.x / a.n_splits, split = blockIdx.x - req * a.n_splits, c0 = blockIdx.y * TILE, range = blockIdx.z, panel0 = range * TREE_RANGE;
-  // shared memory: ring | descriptors | maxima [2][4 parts][128 rows] | barriers
+  // shared memory: ring | scores [128 tokens][columns of a box] | descriptors | maxima [2][4 parts][128 rows] | barriers
   const uint32_t sRing = smem_addr(smem_raw);
   const bool misaligned = (sRing & 1023u) != 0;                 // operand tiles need 1024-byte alignment for the swizzle
-  int4* s_meta = reinterpret_cast<int4*>(smem_raw + TV_STAGES * TV_STAGE);
+  const float* s_scores = reinterpret_cast<const float*>(smem_raw + TV_STAGES * TV_STAGE);
+  const uint32_t sScores = sRing + TV_STAGES * TV_STAGE;
+  int4* s_meta = reinterpret_cast<int4*>(smem_raw + TV_STAGES * TV_STAGE + TV_SCORES);
   float* s_max = reinterpret_cast<float*>(s_meta + TV_META);
   unsigned char* tail = reinterpret_cast<unsigned char*>(s_max + 2 * 4 * TILE);
   const uint32_t bars = smem_addr(tail);
-  const uint32_t full = bars, empty = full + 8 * TV_STAGES, p_full = empty + 8 * TV_STAGES, p_done = p_full + 8;
-  uint32_t* s_tmem_base = reinterpret_cast<uint32_t*>(tail + 8 * (2 * TV_STAGES + 2));
+  const uint32_t full = bars, empty = full + 8 * TV_STAGES, p_full = empty + 8 * TV_STAGES, p_done = p_full + 8, sc_full = p_done + 8, sc_empty = sc_full + 8;
+  uint32_t* s_tmem_base = reinterpret_cast<uint32_t*>(tail + 8 * (2 * TV_STAGES + 4));
   volatile int* abort_flag = reinterpret_cast<int*>(s_tmem_base + 1);
   volatile int* s_count = abort_flag + 1;                       // [2] tiles of the chunk that reach the range, widest class of the split
   if (tid == 0) {
     for (int i = 0; i < TV_STAGES; ++i) { mbar_init(full + 8 * i, 1); mbar_init(empty + 8 * i, 1); }
     mbar_init(p_full, 16);
     mbar_init(p_done, 1);
+    mbar_init(sc_full, 1);
+    mbar_init(sc_empty, 16);
     *abort_flag = misaligned ? 1 : 0;
     s_count[1] = 0;
     mbar_init_fence();
@@ -176,6 +182,22 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
           }
         }
         __syncwarp();
+      } else if (warp == 2) {
+        // ------------------------------------------------------------- TMA producer of the scores, a tile ahead of the weights
+        if (elect_one()) {
+          if (k0 == 0) { tma_prefetch_desc(&map_scores); tma_prefetch_desc(&map_score_boxes); }
+          for (int i = 0; i < cn && ok; ++i, ++k) {
+            const int4 m = s_meta[i];
+            const int nb = vtile_boxes(m.z);
+            if (!(ok = mbar_wait_thin(sc_empty, (k & 1u) ^ 1u, abort_flag))) break;
+            mbar_expect_tx(sc_full, (uint32_t)(nb * JOINT_ROWS * a.v_box * 4));
+            if (nb == TILE / JOINT_ROWS) tma_load_2d(sScores, &map_scores, sc_full, c0, m.x * TILE);
+            else
+              for (int b = 0; b < nb; ++b) tma_load_2d(sScores + b * (uint32_t)(JOINT_ROWS * a.v_box * 4), &map_score_boxes, sc_full, c0, m.x * TILE + b * JOINT_ROWS);
+          }
+          if (!ok && k > 0) mbar_wait_drain(sc_full, (k - 1) & 1u);
+        }
+        __syncwarp();
       }
       __syncthreads();                                          // the descriptors may be replaced
       ok = ok && !*abort_flag;
@@ -192,23 +214,24 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     for (int k0 = 0; k0 < n_mine; k0 += TV_META) {
       __syncthreads();
       const int cn = s_count[0];
-      // Rows of the tile that hold no token, and columns past the last, count as -inf.
-      auto read = [&](int i, float (&x)[32]) {
-        const int4 m = i < cn ? s_meta[i] : make_int4(0, 0, 0, 0);
-        const float* p = a.scores + ((size_t)m.x * TILE + part * 32) * a.C + c0 + row;
-        const int left = in ? m.z - part * 32 : 0;
-        if (left >= 32) {
-#pragma unroll
-          for (int u = 0; u < 32; ++u) x[u] = p[(size_t)u * a.C];
-        } else {
-#pragma unroll
-          for (int u = 0; u < 32; ++u) x[u] = u < left ? p[(size_t)u * a.C] : -INFINITY;
-        }
-      };
-      float x[32];
-      read(0, x);
       for (int i = 0; i < cn; ++i, ++k) {
         const int4 m = s_meta[i];
+        // rows of the tile that hold no token, and columns past the last, count as -inf
+        float x[32];
+        bool got = __all_sync(0xffffffffu, mbar_wait(sc_full, k & 1u, abort_flag));
+        {
+          const float* p = s_scores + part * 32 * a.v_box + row;
+          const int left = in ? m.z - part * 32 : 0;
+          if (left >= 32) {
+#pragma unroll
+            for (int u = 0; u < 32; ++u) x[u] = p[u * a.v_box];
+          } else {
+#pragma unroll
+            for (int u = 0; u < 32; ++u) x[u] = u < left ? p[u * a.v_box] : -INFINITY;
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sc_empty);                     // the next tile's may come
         // the tile's maximum of the row, from the four threads that share it
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -218,7 +241,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         float* const sm = s_max + (k & 1u) * 4 * TILE + row;
         sm[part * TILE] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         // a wait that ran out in one warp ends the loop in the four of its quarter, here: none is left at a barrier
-        if (!(ok = named_bar_and(1 + quarter, 128, ok))) break;
+        if (!(ok = named_bar_and(1 + quarter, 128, ok && got))) break;
         const float most = fmaxf(fmaxf(sm[0], sm[TILE]), fmaxf(sm[2 * TILE], sm[3 * TILE])) * scale;
         const bool grow = most > top + 8.f;                       // also the first finite maximum
         const float next = grow ? most : top, f = next == top ? 1.f : tv_ex2(top - next);      // 0 where there was none yet
@@ -238,7 +261,6 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
           l_sum2 = tv_add2(l_sum2, p);
           split_pair_16<BF16>(p, hi[u >> 1], lo[u >> 1]);
         }
-        read(i + 1, x);                                           // on its way while the products of the tile before are waited for
         if (k > 0) {
           ok = __all_sync(0xffffffffu, mbar_wait(p_done, (k - 1) & 1u, abort_flag));
           fence_after_sync();
@@ -317,7 +339,7 @@ cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, const TreeMap
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TV_SMEM);
   if (e != cudaSuccess) return e;
   e = launch_chained(kernel, dim3(a.n_req * a.n_splits, (a.C + TILE - 1) / TILE, (v.NC + TREE_RANGE - 1) / TREE_RANGE), dim3(TV_THREADS), dim3(1), TV_SMEM, st,
-                     maps.blocks, maps.boxes, maps.node_boxes, v, a);
+                     maps.blocks, maps.boxes, maps.node_boxes, maps.scores, maps.score_boxes, v, a);
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaGetLastError();
