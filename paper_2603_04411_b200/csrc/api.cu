@@ -960,13 +960,15 @@ twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* 
     const uint64_t node_rows = (uint64_t)a.n_req * v.NC * TREE_PANEL_ROWS;
     a.q_box = tree_query_box(a);
     a.v_box = std::min(a.C, TILE);
+    a.m_cluster = tree_merge_cluster(v, a, c->sm_count);
+    a.m_comps = tree_merge_comps(v.d_kv, a.m_cluster);
     const uint64_t score_rows = (uint64_t)a.n_req * (v.TPS + 1) * TILE;
     if (!make_tmap_2d_f32(&maps.scores, a.scores, score_rows, (uint64_t)a.C, TILE, (uint32_t)a.v_box) ||
         !make_tmap_2d_f32(&maps.score_boxes, a.scores, score_rows, (uint64_t)a.C, JOINT_ROWS, (uint32_t)a.v_box)) return TWKV_ERR_CUDA;
     if (!make_tmap_2d(&maps.nodes, a.nk, node_rows, PANEL, PANEL * 2, TILE) || !make_tmap_2d(&maps.node_boxes, a.nv, node_rows, PANEL, PANEL * 2, JOINT_ROWS) ||
         !make_tmap_2d(&maps.uinvT, c->pool + c->off.prep_uinvT + (size_t)layer * v.d_kv * v.d_kv * 2, (uint64_t)v.NC * v.d_kv, PANEL, PANEL * 2, HEAD_DIM / 2) ||
         !make_tmap_2d(&maps.q, a.qop, (uint64_t)a.n_req * v.Hkv * a.Rp, HEAD_DIM, HEAD_DIM * 2, (uint32_t)a.q_box) ||
-        !make_tmap_2d(&maps.uv, c->params[layer].Uinv_v, (uint64_t)v.d_kv, (uint64_t)v.d_kv, (uint64_t)v.d_kv * 2, (uint32_t)v.d_kv / 8)) return TWKV_ERR_CUDA;
+        !make_tmap_2d(&maps.uv, c->params[layer].Uinv_v, (uint64_t)v.d_kv, (uint64_t)v.d_kv, (uint64_t)v.d_kv * 2, (uint32_t)a.m_comps)) return TWKV_ERR_CUDA;
     if (launch_tree_score(v, a, maps, layer, n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
     if (launch_tree_value(v, a, maps, st) != cudaSuccess) return TWKV_ERR_CUDA;
     if (launch_tree_merge(v, a, maps, st) != cudaSuccess) return TWKV_ERR_CUDA;

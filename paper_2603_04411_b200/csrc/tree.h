@@ -34,6 +34,7 @@ struct TreeCall {
   int n_splits;
   int entries;          // room of a request in the K list
   int q_box;            // rows of qop that a CTA takes at a time
+  int m_cluster, m_comps;     // CTAs of a cluster of the merge, components that each takes at a time
   int v_box;            // score columns that a CTA of the value kernel takes, at most 128
   // workspace
   unsigned short* qop;  // [n_req][Hkv][Rp][128] f16 queries in the order of the score contraction
@@ -52,7 +53,7 @@ struct TreeCall {
 };
 
 // The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the
-// queries, U_V^-1 (an eighth of its rows, 64 columns), the
+// queries, U_V^-1 (m_comps rows, 64 columns), the
 // scores (a tile's rows or sixteen of them, v_box columns).
 struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q, uv, scores, score_boxes; };
 
@@ -75,6 +76,8 @@ cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int
 cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, const TreeMaps& maps, int layer, int n_pieces, cudaStream_t st);
 int tree_max_pairs(int sm_count);
 int tree_query_box(const TreeCall& a);
+int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count);
+int tree_merge_comps(int d_kv, int cl);
 cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);
 cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);
 

@@ -1,11 +1,13 @@
 // End of tree attention: sum of the splits, division by the sum of the weights, projection out_h = (acc_h / l_h) U_V^-1[:, head slice].
 //
-// A cluster of eight CTAs per (128 rows, KV head): row = (request, node; head of the group), and CTA c takes the spectral components
-// [c d/8, (c + 1) d/8).  It sums their splits, each relative to its own maximum, normalises, and makes them the A operand of a tcgen05 product with its rows of U_V^-1
-// (as they lie: MN-major B): two 16-bit parts of the cache type per component, fp32 accumulation in tensor memory.  The eight partial
-// products meet in distributed shared memory, 16 columns per CTA.  What bounds it is the way of the partial sums (4 d_kv bytes per row and
-// split) into the SMs, and for few rows the chain of reads; the decode merge does the product by FMAs, which for hundreds of nodes cost
-// several times the reads (256 nodes of 32 heads 373 us by a CTA per row).
+// A cluster of CL CTAs per (128 rows, KV head): row = (request, node; head of the group), and CTA c takes the spectral components
+// [c d/CL, (c + 1) d/CL), up to 128 at a time.  It sums their splits, each relative to its own maximum, normalises, and makes them the A operand of
+// a tcgen05 product with its rows of U_V^-1 (as they lie: MN-major B): two 16-bit parts of the cache type per component, fp32 accumulation in
+// tensor memory.  The CL partial products meet in distributed shared memory, 128 / CL columns per CTA.
+// What bounds it is the way of the partial sums (4 d_kv bytes per row and split) into the SMs, and for few rows the chain of reads, which a
+// cluster of eight shortens; with many rows the exchange would cost more than the rest (64 KiB per CTA of eight), so CL is the largest that leaves
+// two CTAs per SM.  The decode merge does the product by FMAs, which for hundreds of nodes cost several times the reads (256 nodes of 32
+// heads 373 us by a CTA per row).
 // chain_start() stands behind the allocation of tensor memory: two CTAs of this kernel share an SM, so the next kernel of the chain must
 // not find columns free that one of them still needs.
 #include "twkv_dev.h"
@@ -16,30 +18,30 @@
 namespace twkv {
 using namespace tc;
 
-constexpr int TM_THREADS = 256, TM_CL = 8;
+constexpr int TM_THREADS = 256;
 constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 components] of one part
 constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // high and low parts of up to 128 components; their rows of U_V^-1, 128 columns
 constexpr int TM_FEW = 4;                                     // splits whose weights are looked up once per row
-constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16 + TM_FEW * 2 * 4 + TM_FEW) + 64;
+constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16 + TM_FEW * 3 * 4 + TM_FEW) + 64;
 static_assert(2 * TM_SMEM <= 228 * 1024 - 2 * 1024, "two CTAs per SM");
-static_assert(TM_CL * TILE * (HEAD_DIM / TM_CL) * 4 <= TM_A, "the partial products arrive where the A operand was");
+static_assert(TILE * HEAD_DIM * 4 <= TM_A, "the partial products arrive where the A operand was");
 
 __device__ __forceinline__ float tm_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
-template <bool BF16>
+template <bool BF16, int CL>
 __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
   float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE, *s_w = s_inv + TILE;      // per row
-  int4* s_row = reinterpret_cast<int4*>(s_w + TILE * TM_FEW * 2);                     // first part, splits, request, row of the outputs; -1: none
+  int4* s_row = reinterpret_cast<int4*>(s_w + TILE * TM_FEW * 3);                     // first part, splits, request, row of the outputs; -1: none
   unsigned char* s_cls = reinterpret_cast<unsigned char*>(s_row + TILE);
   unsigned char* tail = s_cls + TILE * TM_FEW;
   const uint32_t b_full = smem_addr(tail), done = b_full + 8;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(tail + 16);
   volatile int* abort_flag = reinterpret_cast<int*>(s_tmem + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int c = (int)cluster_cta_rank(), g = blockIdx.y, rep = v.rep, jn = v.d_kv / TM_CL, j0 = c * jn;      // jn: a multiple of 16, at most 128
-  const int slot0 = (blockIdx.x / TM_CL) * (TILE / rep), n_slots = a.n_req * a.T;
+  const int c = CL > 1 ? (int)cluster_cta_rank() : 0, g = blockIdx.y, rep = v.rep, jn = a.m_comps;      // components at a time: a multiple of 16, at most 128
+  const int slot0 = (blockIdx.x / CL) * (TILE / rep), n_slots = a.n_req * a.T;
   const bool misaligned = (sA & 1023u) != 0;
   if (tid == 0) {
     mbar_init(b_full, 1);
@@ -54,17 +56,9 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   chain_start();
   const uint32_t tmem = *s_tmem;
   chain_wait();
-  if (warp == 0 && elect_one() && !misaligned) {               // on its way while the splits are summed
-    mbar_expect_tx(b_full, (uint32_t)jn * 256u);
-    tma_load_2d(sB, &map_uv, b_full, g * HEAD_DIM, j0);
-    tma_load_2d(sB + jn * 128u, &map_uv, b_full, g * HEAD_DIM + 64, j0);
-  }
-  __syncwarp();
-
   // A thread per row (slot, h), slot = request * T + node: where its parts are, the largest reference of its splits, one over the sum of all weights;
   // and what the parts of the first splits are worth.  The components of a range of panels have a reference of their own; behind a split's
   // widest class there are none.  Looked up here once, so that the reads below depend on shared memory only.
-  const int range0 = j0 / (TREE_RANGE * PANEL);               // of the CTA's first components; a later one may lie in the next range
   if (tid < TILE) {
     const int slot = slot0 + tid / rep, req = slot / a.T, t = slot - req * a.T;
     int row = -1, used = 0;
@@ -87,10 +81,10 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
         if (used <= TM_FEW) {
 #pragma unroll
           for (int k = 0; k < TM_FEW; ++k) {
-            const float r0 = range0 == 0 ? y[k].x : range0 == 1 ? y[k].y : y[k].z, r1 = range0 == 0 ? y[k].y : y[k].z;
             s_cls[tid * TM_FEW + k] = k < used ? (unsigned char)a.part_cls[req * a.n_splits + k] : 0;
-            s_w[(tid * TM_FEW + k) * 2] = r0 == -INFINITY ? 0.f : tm_ex2(r0 - m);
-            s_w[(tid * TM_FEW + k) * 2 + 1] = r1 == -INFINITY ? 0.f : tm_ex2(r1 - m);
+            const float ref[3] = {y[k].x, y[k].y, y[k].z};
+#pragma unroll
+            for (int e = 0; e < 3; ++e) s_w[(tid * TM_FEW + k) * 3 + e] = ref[e] == -INFINITY ? 0.f : tm_ex2(ref[e] - m);
           }
         }
       }
@@ -102,7 +96,6 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   __syncthreads();
   // Sums: a warp takes rows warp, warp + 8, ..., its lanes four components.  Eight reads on their way: of as many rows where a row has few splits, of
   // eight splits otherwise.  (16384 rows of one split one after the other took 204 us.)
-  const int comp = j0 + lane * 4, range = comp / (TREE_RANGE * PANEL);
   const bool mine = lane * 4 < jn;
   auto put = [&](int r, float4 x) {                             // a row's normalised components as the A operand
     if (!mine) return;
@@ -118,84 +111,98 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     *reinterpret_cast<uint2*>(d) = make_uint2(hi[0], hi[1]);
     *reinterpret_cast<uint2*>(d + 2 * TM_PANEL) = make_uint2(lo[0], lo[1]);
   };
-  const float* const acc = a.part_acc + comp;
-  if (a.n_splits <= TM_FEW) {
-#pragma unroll 1
-    for (int b = 0; b < TILE / 8; b += 8) {
-      float4 x[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-      for (int s = 0; s < a.n_splits; ++s) {
-        float4 y[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int r = warp + 8 * (b + k);
-          const int4 q = s_row[r];
-          const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
-          y[k] = in ? *reinterpret_cast<const float4*>(acc + (size_t)(q.x + s * v.Hq) * v.d_kv) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int r = warp + 8 * (b + k);
-          const int4 q = s_row[r];
-          const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
-          const float w = in ? s_w[(r * TM_FEW + s) * 2 + range - range0] : 0.f;
-          x[k].x += y[k].x * w; x[k].y += y[k].y * w; x[k].z += y[k].z * w; x[k].w += y[k].w * w;
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) put(warp + 8 * (b + k), x[k]);
-    }
-  } else {
-#pragma unroll 1
-    for (int r = warp; r < TILE; r += TM_THREADS / 32) {
-      const int4 q = s_row[r];
-      if (q.x < 0) continue;
-      const int* cls = a.part_cls + q.z * a.n_splits;
-      const float* refs = reinterpret_cast<const float*>(a.part_ml + q.x) + range;
-      const float most = s_most[r];
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-      for (int s0 = 0; s0 < q.y; s0 += 8) {
-        float4 y[8];
-        float ref[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const bool in = mine && s0 + k < q.y && comp < cls[s0 + k] * PANEL;
-          y[k] = in ? *reinterpret_cast<const float4*>(acc + (size_t)(q.x + (s0 + k) * v.Hq) * v.d_kv) : make_float4(0.f, 0.f, 0.f, 0.f);
-          ref[k] = in ? refs[(size_t)(s0 + k) * v.Hq * 4] : -INFINITY;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float w = ref[k] == -INFINITY ? 0.f : tm_ex2(ref[k] - most);
-          x.x += y[k].x * w; x.y += y[k].y * w; x.z += y[k].z * w; x.w += y[k].w * w;
-        }
-      }
-      put(r, x);
-    }
-  }
-  fence_proxy_async_smem();
-  __syncthreads();
   bool ok = !misaligned;
-  if (warp == 0 && elect_one() && ok) {
-    if (mbar_wait(b_full, 0u, abort_flag)) {
-      fence_after_sync();
-      constexpr uint32_t idesc = idesc_f16(BF16 ? 1 : 0, 128, 128) | (1u << 16);       // B MN-major
-      const uint32_t b_lo = ((sB >> 4) & 0x3fffu) | ((uint32_t)(jn * 128) >> 4 << 16);
-      for (int part = 1; part >= 0; --part)                     // the low parts first: the sum is cut after every instruction
-        for (int ks = 0; ks < jn / 16; ++ks) {
-          const uint32_t a_lo = kmajor_sw128_desc_lo(sA + part * 2 * TM_PANEL + (ks >> 2) * TM_PANEL) + 2 * (ks & 3);
-          mma_f16_ss(tmem, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | a_lo, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u), idesc,
-                     part == 0 || ks > 0 ? 1u : 0u);
-        }
-      mma_commit(done);
+  uint32_t ph = 0;
+  const int first = c * (v.d_kv / CL), n_chunks = v.d_kv / CL / jn;
+  for (int chunk = 0; chunk < n_chunks; ++chunk) {
+    const int j0 = first + chunk * jn, comp = j0 + lane * 4, range = comp / (TREE_RANGE * PANEL);
+    if (warp == 0 && elect_one() && ok) {                      // U_V^-1, on its way while the splits are summed
+      mbar_expect_tx(b_full, (uint32_t)jn * 256u);
+      tma_load_2d(sB, &map_uv, b_full, g * HEAD_DIM, j0);
+      tma_load_2d(sB + jn * 128u, &map_uv, b_full, g * HEAD_DIM + 64, j0);
     }
+    __syncwarp();
+    const float* const acc = a.part_acc + comp;
+    if (a.n_splits <= TM_FEW) {
+#pragma unroll 1
+      for (int b = 0; b < TILE / 8; b += 8) {
+        float4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int s = 0; s < a.n_splits; ++s) {
+          float4 y[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int r = warp + 8 * (b + k);
+            const int4 q = s_row[r];
+            const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
+            y[k] = in ? *reinterpret_cast<const float4*>(acc + (size_t)(q.x + s * v.Hq) * v.d_kv) : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const int r = warp + 8 * (b + k);
+            const int4 q = s_row[r];
+            const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
+            const float w = in ? s_w[(r * TM_FEW + s) * 3 + range] : 0.f;
+            x[k].x += y[k].x * w; x[k].y += y[k].y * w; x[k].z += y[k].z * w; x[k].w += y[k].w * w;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) put(warp + 8 * (b + k), x[k]);
+      }
+    } else {
+#pragma unroll 1
+      for (int r = warp; r < TILE; r += TM_THREADS / 32) {
+        const int4 q = s_row[r];
+        if (q.x < 0) continue;
+        const int* cls = a.part_cls + q.z * a.n_splits;
+        const float* refs = reinterpret_cast<const float*>(a.part_ml + q.x) + range;
+        const float most = s_most[r];
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int s0 = 0; s0 < q.y; s0 += 8) {
+          float4 y[8];
+          float ref[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const bool in = mine && s0 + k < q.y && comp < cls[s0 + k] * PANEL;
+            y[k] = in ? *reinterpret_cast<const float4*>(acc + (size_t)(q.x + (s0 + k) * v.Hq) * v.d_kv) : make_float4(0.f, 0.f, 0.f, 0.f);
+            ref[k] = in ? refs[(size_t)(s0 + k) * v.Hq * 4] : -INFINITY;
+          }
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float w = ref[k] == -INFINITY ? 0.f : tm_ex2(ref[k] - most);
+            x.x += y[k].x * w; x.y += y[k].y * w; x.z += y[k].z * w; x.w += y[k].w * w;
+          }
+        }
+        put(r, x);
+      }
+    }
+    fence_proxy_async_smem();
+    __syncthreads();
+    if (warp == 0 && elect_one() && ok) {
+      if (mbar_wait(b_full, ph, abort_flag)) {
+        fence_after_sync();
+        constexpr uint32_t idesc = idesc_f16(BF16 ? 1 : 0, 128, 128) | (1u << 16);       // B MN-major
+        const uint32_t b_lo = ((sB >> 4) & 0x3fffu) | ((uint32_t)(jn * 128) >> 4 << 16);
+        for (int part = 1; part >= 0; --part)                     // the low parts first: the sum is cut after every instruction
+          for (int ks = 0; ks < jn / 16; ++ks) {
+            const uint32_t a_lo = kmajor_sw128_desc_lo(sA + part * 2 * TM_PANEL + (ks >> 2) * TM_PANEL) + 2 * (ks & 3);
+            mma_f16_ss(tmem, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | a_lo, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u), idesc,
+                       chunk > 0 || part == 0 || ks > 0 ? 1u : 0u);
+          }
+        mma_commit(done);
+      }
+    }
+    __syncwarp();
+    ok = ok && __all_sync(0xffffffffu, mbar_wait(done, ph, abort_flag));      // (the operands may be replaced)
+    ph ^= 1u;
+    fence_after_sync();
+    __syncthreads();
   }
-  __syncwarp();
-  ok = ok && __all_sync(0xffffffffu, mbar_wait(done, 0u, abort_flag));
-  fence_after_sync();
-  cluster_sync_all();                                           // every CTA's A operand has been used: the parts may arrive there
+  constexpr int CW = HEAD_DIM / CL;                             // columns a CTA writes
+  if constexpr (CL > 1) cluster_sync_all();                     // every CTA's A operand has been used: the parts may arrive there
   {
     const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
     float x[32];
@@ -209,58 +216,94 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
 #pragma unroll
         for (int e = 0; e < 32; ++e) x[e] = 0.f;
       }
+      // four columns to the CTA that writes them: [from][four columns][row], so that a warp's rows lie together
 #pragma unroll
-      for (int e = 0; e < 32; e += 4)                           // to the CTA that writes these columns
-        st_cluster_f32x4(cluster_map(sA + (uint32_t)((c * TILE + row) * 64 + (e & 15) * 4), (uint32_t)((col + e) >> 4)), make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]));
+      for (int e = 0; e < 32; e += 4) {
+        const uint32_t at = sA + (uint32_t)(((c * CW + (col + e) % CW) / 4 * TILE + row) * 16);
+        const float4 w = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+        if constexpr (CL > 1) st_cluster_f32x4(cluster_map(at, (uint32_t)((col + e) / CW)), w);
+        else *reinterpret_cast<float4*>(smem + (at - sA)) = w;
+      }
     }
   }
   fence_before_sync();
-  cluster_sync_all();                                           // every part has arrived; nothing remote is touched from here on
+  if constexpr (CL > 1) cluster_sync_all();                     // every part has arrived; nothing remote is touched from here on
+  else __syncthreads();
   fence_after_sync();
   if (warp == 1) tmem_dealloc(tmem, 128);
   {
-    const int r = tid >> 1, e0 = (tid & 1) * 8;
+    const int r = tid & (TILE - 1), e0 = (tid >> 7) * (CW / 2);
     const int4 q = s_row[r];
     if (q.w >= 0) {
-      const float* in = reinterpret_cast<const float*>(smem) + r * 16 + e0;
-      float o[8];
+      const bool bad = q.y > 0 && (a.masks[q.w] & a.bad[q.z]);    // sees a node whose value is not finite
+#pragma unroll 2
+      for (int e1 = e0; e1 < e0 + CW / 2; e1 += 8) {
+        float o[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = 0.f;
+        for (int e = 0; e < 8; ++e) o[e] = 0.f;
 #pragma unroll
-      for (int k = 0; k < TM_CL; ++k) {                         // fixed order
-        const float4 x = *reinterpret_cast<const float4*>(in + k * TILE * 16), y = *reinterpret_cast<const float4*>(in + k * TILE * 16 + 4);
-        o[0] += x.x; o[1] += x.y; o[2] += x.z; o[3] += x.w; o[4] += y.x; o[5] += y.y; o[6] += y.z; o[7] += y.w;
-      }
-      if (q.y > 0 && (a.masks[q.w] & a.bad[q.z])) {  // sees a node whose value is not finite
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = __int_as_float(0x7fffffff);
-      }
-      const size_t at = ((size_t)q.w * v.Hq + g * rep + r % rep) * HEAD_DIM + c * 16 + e0;
-      if (v.out_dtype == TWKV_F32) {
-        float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at);
-        d[0] = make_float4(o[0], o[1], o[2], o[3]);
-        d[1] = make_float4(o[4], o[5], o[6], o[7]);
-      } else {
-        unsigned w[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (v.out_dtype == TWKV_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(o[2 * k + 1]), "f"(o[2 * k]));
-          else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(o[2 * k + 1]), "f"(o[2 * k]));
+        for (int k = 0; k < CL; ++k) {                            // fixed order
+          const float4* in = reinterpret_cast<const float4*>(smem) + (k * CW + e1) / 4 * TILE + r;
+          const float4 x = in[0], y = in[TILE];
+          o[0] += x.x; o[1] += x.y; o[2] += x.z; o[3] += x.w; o[4] += y.x; o[5] += y.y; o[6] += y.z; o[7] += y.w;
         }
-        *reinterpret_cast<uint4*>(reinterpret_cast<unsigned short*>(a.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+        if (bad) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] = __int_as_float(0x7fffffff);
+        }
+        const size_t at = ((size_t)q.w * v.Hq + g * rep + r % rep) * HEAD_DIM + c * CW + e1;
+        if (v.out_dtype == TWKV_F32) {
+          float4* d = reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at);
+          d[0] = make_float4(o[0], o[1], o[2], o[3]);
+          d[1] = make_float4(o[4], o[5], o[6], o[7]);
+        } else {
+          unsigned w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (v.out_dtype == TWKV_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(o[2 * k + 1]), "f"(o[2 * k]));
+            else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(o[2 * k + 1]), "f"(o[2 * k]));
+          }
+          *reinterpret_cast<uint4*>(reinterpret_cast<unsigned short*>(a.out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
       }
     }
   }
   if (tid == 0 && *abort_flag) set_status(v, misaligned ? TWKV_ERR_DEVICE_CHECK : TWKV_ERR_TIMEOUT);
 }
 
-cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
-  ProfScope ps(TWKV_K_MERGE, st);
-  auto kernel = v.dtype == TWKV_BF16 ? tree_merge_kernel<true> : tree_merge_kernel<false>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TM_SMEM);
+// CTAs of a cluster: as many as leave two CTAs per SM.
+int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count) {
+  const int work = (a.n_req * a.T * v.rep + TILE - 1) / TILE * v.Hkv;
+  int cl = 8;
+  while (cl > 1 && work * cl > 2 * sm_count) cl /= 2;
+  return cl;
+}
+// Components that a CTA takes at a time: the least number of equal pieces of at most 128, a multiple of sixteen each.
+int tree_merge_comps(int d_kv, int cl) {
+  int n = (d_kv / cl + 127) / 128;
+  while (d_kv / cl % (16 * n)) ++n;
+  return d_kv / cl / n;
+}
+
+template <bool BF16, int CL>
+static cudaError_t launch_tree_merge_t(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(tree_merge_kernel<BF16, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TM_SMEM);
   if (e != cudaSuccess) return e;
   const int tiles = (a.n_req * a.T * v.rep + TILE - 1) / TILE;
-  e = launch_chained(kernel, dim3(TM_CL * tiles, v.Hkv), dim3(TM_THREADS), dim3(TM_CL), TM_SMEM, st, maps.uv, v, a);
+  return launch_chained(tree_merge_kernel<BF16, CL>, dim3(CL * tiles, v.Hkv), dim3(TM_THREADS), dim3(CL), TM_SMEM, st, maps.uv, v, a);
+}
+template <bool BF16>
+static cudaError_t launch_tree_merge_cl(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
+  switch (a.m_cluster) {
+    case 1: return launch_tree_merge_t<BF16, 1>(v, a, maps, st);
+    case 2: return launch_tree_merge_t<BF16, 2>(v, a, maps, st);
+    case 4: return launch_tree_merge_t<BF16, 4>(v, a, maps, st);
+    default: return launch_tree_merge_t<BF16, 8>(v, a, maps, st);
+  }
+}
+cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
+  ProfScope ps(TWKV_K_MERGE, st);
+  const cudaError_t e = v.dtype == TWKV_BF16 ? launch_tree_merge_cl<true>(v, a, maps, st) : launch_tree_merge_cl<false>(v, a, maps, st);
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaGetLastError();
