@@ -21,10 +21,13 @@
 namespace twkv {
 
 // Estimated cycles of an item of the score kernel: per KV head and pass a part for rotation and score products, which grow with the query rows, beyond
-// 64 with the stores of the scores; and a part per panel.  Fitted to lists of one class (16 to 512 query rows, 1 to 16 panels).  Only the ratios matter.
+// 64 with the stores of the scores; and a part per panel, more of it where the panels are brought once per KV head.  Fitted to lists of one class
+// (16 to 512 query rows, 1 to 16 panels).  Only the ratios matter.
 __device__ __forceinline__ unsigned tree_cost(const DevView& v, const TreeCall& a, int cls) {
-  const unsigned rows = 14u * (unsigned)min(a.R, 64) + 28u * (unsigned)max(a.R - 64, 0), passes = cls > 8 ? 2u : 1u;
-  return (unsigned)v.Hkv * (passes * (1500u + rows) + 300u * (unsigned)cls);
+  const unsigned rows = 14u * (unsigned)min(a.R, 64) + 28u * (unsigned)max(a.R - 64, 0);
+  if (cls <= 8) return (unsigned)v.Hkv * (1500u + rows + 300u * (unsigned)cls);
+  if (a.R > 64) return (unsigned)v.Hkv * (1500u + rows + 500u * (unsigned)cls);
+  return (unsigned)v.Hkv * (3000u + 3u * rows + 300u * (unsigned)cls);
 }
 
 // Refuses a request whose sequence an earlier one names, or into whose rows an earlier one reaches: those are not its to write (the

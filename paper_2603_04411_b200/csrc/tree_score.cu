@@ -17,7 +17,7 @@
 //   warps 4-11  rotation and high / low split (thread = one token row x half of the RoPE frequencies)
 //   warps 12-15 scores out: masked (nodes), stored in the order of the V tiles (thread = one token row)
 // Scores are stored without their scale, which the value kernel's exponents carry (a negative scale is in the queries).
-// A class wider than eight panels runs as two passes over its panels, the second adding to the scores the first one stored (one addition
+// A class wider than eight panels runs as two passes over its panels (unless there are many query rows, see panels()), the second adding to the scores the first one stored (one addition
 // per score, in memory: its order cannot vary).
 // All waits are bounded (tc_util.cuh); a wait that runs out ends the kernel with TWKV_ERR_TIMEOUT.
 #include "twkv_dev.h"
@@ -31,6 +31,7 @@ constexpr int TS_THREADS = 512;
 constexpr int TS_REGS_LIGHT = 56, TS_REGS_EPI = 184, TS_REGS_OUT = 88;      // 128 x 56 + 256 x 184 + 128 x 88 = 65536
 constexpr int TS_A_SLOTS = 8, TS_B_STAGES = 4, TS_SLABS = 3;
 constexpr int TS_Q_STAGES = 6;                                  // stages of the query ring where a block has at most 32 rows, half as many where it has 64
+constexpr int TS_STREAM_ROWS = 64;                              // query rows beyond which a class of more than eight panels is rebuilt in one pass
 constexpr int TS_S_SLOTS = 4;                                   // score accumulators of 32 columns, or half as many of 64
 constexpr uint32_t TS_PANEL = 16384, TS_B_PART = 8192, TS_B_STAGE = 2 * TS_B_PART;
 constexpr int TS_QCOLS = 64;                                    // query rows of a block, half of them in each CTA
@@ -129,6 +130,9 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     }
     return u;
   };
+  // panels of a pass: eight, which stay in their ring slots for all KV heads of the unit; all, brought once per KV head, where a class is wider and
+  // there are so many query rows that rotating, multiplying and storing twice costs more
+  auto panels = [&](int cls) -> int { return a.R > TS_STREAM_ROWS && cls > TS_A_SLOTS ? cls : TS_A_SLOTS; };
   // K slot of a row of an entry in the cache, -1 where it holds no token
   auto cache_slot = [&](const int4& e, int row) -> int {
     if (e.x < 0) return v.joint_rows()[(size_t)~e.x * TILE + row];
@@ -154,8 +158,8 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         tma_prefetch_desc(&map_boxes);
         tma_prefetch_desc(&map_nodes);
         tma_prefetch_desc(&map_q);
-        // panels: unit w, panel j, panels so far ak (slot = ak % 8); blocks: unit lw, first panel of the pass lp, KV head lsl, block lsub
-        int w = w0, j = 0, lw = w0, lp = 0, lsl = 0, lsub = 0;
+        // panels: unit w, panel j, times the unit's panels have been brought, panels so far ak (slot = ak % 8); blocks: unit lw, first panel of the pass lp, KV head lsl, block lsub
+        int w = w0, j = 0, again = 0, lw = w0, lp = 0, lsl = 0, lsub = 0;
         uint32_t ak = 0, lst = 0, lph = 0, idle = 0;
         TsUnit u = unit(w0), lu = u;
         while (w < total || lw < total) {
@@ -178,7 +182,12 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
               tma_load_2d_pair(dst, &map_blocks, a_full_even + 8 * slot, 0, j < own ? (u.e.z + j) * TILE : v.n_blocks * TILE);
             }
             ++ak;
-            if (++j == u.cls) { j = 0; u = unit(++w); }
+            if (++j == u.cls) {
+              j = 0;
+              if (panels(u.cls) > TS_A_SLOTS && ++again < nh) continue;         // the panels of a streamed unit's next KV head
+              again = 0;
+              u = unit(++w);
+            }
             moved = true;
           }
           if (lw < total && mbar_test(q_empty + 8 * lst, lph ^ 1u)) {
@@ -192,7 +201,7 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
               lsub = 0;
               if (++lsl == nh) {
                 lsl = 0;
-                lp += TS_A_SLOTS;
+                lp += panels(lu.cls);
                 if (lp >= lu.cls) { lp = 0; lu = unit(++lw); }
               }
             }
@@ -217,8 +226,9 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         for (int w = w0; w < total && ok; ++w) {
           const TsUnit nxt = unit(w + 1);
           const int g0 = first_head(w);
-          for (int p0 = 0; p0 < u.cls && ok; p0 += TS_A_SLOTS) {
-            const int np = min(TS_A_SLOTS, u.cls - p0);
+          const int span = panels(u.cls);
+          for (int p0 = 0; p0 < u.cls && ok; p0 += span) {
+            const int np = min(span, u.cls - p0);
             for (int sl = 0; sl < nh && ok; ++sl) {
               const int g = head(g0, sl);
               for (int j = 0; j < np; j += 2) {
@@ -246,14 +256,16 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         TsUnit u = unit(w0);
         for (int w = w0; w < total && ok; ++w) {
           const TsUnit nxt = unit(w + 1);
-          for (int p0 = 0; p0 < u.cls && ok; p0 += TS_A_SLOTS) {
-            const int np = min(TS_A_SLOTS, u.cls - p0);
+          const int span = panels(u.cls);
+          const bool stream = span > TS_A_SLOTS;
+          for (int p0 = 0; p0 < u.cls && ok; p0 += span) {
+            const int np = min(span, u.cls - p0);
             for (int sl = 0; sl < nh && ok; ++sl) {
               // the buffer is free once the score products over its previous contents have retired
               if (!(ok = mbar_wait_thin(slab_empty + 8 * sbuf, sph ^ 1u, abort_flag))) break;
               fence_after_sync();
               const uint32_t d = tmem_base + TS_COL_SLAB + sbuf * 128;
-              const bool first = sl == 0, last = sl == nh - 1;
+              const bool first = stream || sl == 0, last = stream || sl == nh - 1;
               uint32_t an = ak;
               for (int j = 0; j < np; j += 2, an += 2) {
                 const bool two = j + 1 < np;
@@ -274,8 +286,8 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
               if (!ok) break;
               mma_commit_pair_both(slab_full + 8 * sbuf);
               if (++sbuf == TS_SLABS) { sbuf = 0; sph ^= 1u; }
+              if (last) ak += np;
             }
-            ak += np;
           }
           u = nxt;
         }
@@ -290,7 +302,7 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         TsUnit u = unit(w0);
         for (int w = w0; w < total && ok; ++w) {
           const TsUnit nxt = unit(w + 1);
-          for (int p0 = 0; p0 < u.cls && ok; p0 += TS_A_SLOTS) {
+          for (int p0 = 0; p0 < u.cls && ok; p0 += panels(u.cls)) {
             for (int sl = 0; sl < nh && ok; ++sl) {
               if (!(ok = mbar_wait_thin(kr_full + 8 * sbuf, sph, abort_flag))) break;
               const uint32_t kr = tmem_base + TS_COL_SLAB + sbuf * 128;
@@ -353,7 +365,7 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
       const TsUnit nxt = unit(w + 1);
       [[maybe_unused]] bool has_row = true;
       if constexpr (DBG) has_row = cached(u.e) ? cache_slot(u.e, row) >= 0 : (u.e.y & TREE_NODES) && row < (u.e.y >> 16);
-      const int passes = (u.cls + TS_A_SLOTS - 1) / TS_A_SLOTS;
+      const int passes = u.cls > panels(u.cls) ? 2 : 1;
       const int pos_next = row_pos(nxt.e);                                        // fetched now, used after the tile's slabs
       for (int ps = 0; ps < passes && ok; ++ps) {
         for (int sli = 0; sli < nh; ++sli) {
@@ -426,7 +438,7 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     int srow = score_row(u.e);
     for (int w = w0; w < total && ok; ++w) {
       const TsUnit nxt = unit(w + 1);
-      const int passes = (u.cls + TS_A_SLOTS - 1) / TS_A_SLOTS, g0 = first_head(w);
+      const int passes = u.cls > panels(u.cls) ? 2 : 1, g0 = first_head(w);
       const bool live = srow >= 0;                                 // (a filler's rows are not)
       float* const dst_row = a.scores + (size_t)(live ? srow : 0) * a.C;
       const bool node = (u.e.y & TREE_NODES) != 0;
