@@ -856,7 +856,8 @@ static size_t tree_layout(const twkv_cache* c, TreeCall& a, unsigned char* base)
   a.vcut = (int*)take(n * (a.n_splits + 1) * sizeof(int));
   a.cta_start = (int*)take((MAX_PLAN_CTAS + 1) * sizeof(int));
   a.parts = (int*)take(sizeof(int));
-  a.part_ml = (float4*)take(parts * sizeof(float4));
+  a.part_m = (float4*)take(parts * sizeof(float4));
+  a.part_l = (float*)take(parts * sizeof(float));
   a.part_cls = (int*)take(std::max(n, fill) * sizeof(int));
   a.part_acc = (float*)take(parts * v.d_kv * sizeof(float));
   a.scores = (float*)take(n * tiles * TILE * a.C * sizeof(float));
@@ -870,6 +871,10 @@ static TreeCall tree_shape(const twkv_cache* c, int n_req, int max_nodes) {
   a.n_req = n_req; a.T = max_nodes;
   a.R = max_nodes * v.rep; a.Rs = a.R > 4 ? (a.R + 7) & ~7 : 4; a.Rp = (a.R + 15) & ~15; a.C = v.Hkv * a.Rs;
   a.entries = (v.TPS + 4) & ~1;
+  // Two bf16 parts carry 16 bits: 4e-6 of the outputs, which only fp32 outputs show.  Their bf16 caches take three.
+  a.n_parts = v.dtype == TWKV_BF16 && v.out_dtype == TWKV_F32 ? 3 : 2;
+  a.range = tree_value_range(a.n_parts);
+  a.drain = v.out_dtype == TWKV_F32 ? TREE_DRAIN_F32 : TREE_DRAIN_16;
   a.n_splits = std::max(1, std::min(TREE_MAX_SPLITS, c->sm_count / (n_req * ((a.C + TILE - 1) / TILE))));
   return a;
 }
@@ -961,7 +966,7 @@ twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* 
     a.q_box = tree_query_box(a);
     a.v_box = std::min(a.C, TILE);
     a.m_cluster = tree_merge_cluster(v, a, c->sm_count);
-    a.m_comps = tree_merge_comps(v.d_kv, a.m_cluster);
+    a.m_comps = tree_merge_comps(v.d_kv, a.m_cluster, a.n_parts);
     const uint64_t score_rows = (uint64_t)a.n_req * (v.TPS + 1) * TILE;
     if (!make_tmap_2d_f32(&maps.scores, a.scores, score_rows, (uint64_t)a.C, TILE, (uint32_t)a.v_box) ||
         !make_tmap_2d_f32(&maps.score_boxes, a.scores, score_rows, (uint64_t)a.C, JOINT_ROWS, (uint32_t)a.v_box)) return TWKV_ERR_CUDA;

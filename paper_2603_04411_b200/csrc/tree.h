@@ -10,8 +10,14 @@
 
 namespace twkv {
 
-constexpr int TREE_RANGE = 6;                    // panels whose sums a CTA of the value kernel keeps
-static_assert((TWKV_MAX_CLASSES + TREE_RANGE - 1) / TREE_RANGE <= 3, "three ranges beside the sum of the weights");
+// The tensor core cuts its fp32 sum toward zero after every instruction: an expected loss of half a unit in the last place, 0.36 x 2^-23 of the sum's size
+// (averaged over mantissas), and of the final sum half of that per instruction, whether the sum grows steadily or wanders.  The kernels give that expected loss
+// back as a factor 1 + TREE_CUT x instructions.  Errors of fp32 outputs, without / with it for the keys alone: 4 sequences of 700 tokens 1.3e-6 / 5.2e-7 (plain
+// fp32 sums: 6.8e-7), 2 of 8192 tokens 1.1e-6 / 6.9e-7 (1.7e-6).
+constexpr float TREE_CUT = 2.15e-8f;
+// Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 and 16-bit outputs: what the expectation leaves grows with the chain.
+constexpr int TREE_DRAIN_F32 = 4, TREE_DRAIN_16 = 128;
+constexpr int TREE_MAX_RANGES = 4;               // ranges of panels whose sums a CTA of the value kernel keeps
 constexpr int TREE_MAX_SPLITS = 64;              // of a request's V tiles
 constexpr int TREE_PANEL_ROWS = 64;              // rows of a panel of the nodes' tiles
 static_assert(TWKV_TREE_MAX_NODES <= TREE_PANEL_ROWS && TWKV_TREE_MAX_NODES <= 64, "a node is a bit of a 64-bit word, and a row of a panel");
@@ -35,6 +41,9 @@ struct TreeCall {
   int entries;          // room of a request in the K list
   int q_box;            // rows of qop that a CTA takes at a time
   int m_cluster, m_comps;     // CTAs of a cluster of the merge, components that each takes at a time
+  int n_parts;          // parts that a weight, and a component of the merge, goes into products as
+  int drain;            // tiles that an accumulator of the value kernel takes before it is emptied
+  int range;            // panels whose sums a CTA of the value kernel keeps
   int v_box;            // score columns that a CTA of the value kernel takes, at most 128
   // workspace
   unsigned short* qop;  // [n_req][Hkv][Rp][128] f16 queries in the order of the score contraction
@@ -48,7 +57,8 @@ struct TreeCall {
   int* vcut;            // [n_req][n_splits + 1]
   int *cta_start, *parts;     // [pieces + 1] first item part of a piece; parts of an item
   float* part_acc;      // [n_req][T][n_splits][Hq][d_kv]
-  float4* part_ml;      // [n_req][T][n_splits][Hq] what the split's weights are relative to (powers of two) in each range of panels, their sum
+  float4* part_m;       // [n_req][T][n_splits][Hq] what the split's weights are relative to (powers of two), per range of panels
+  float* part_l;        // [n_req][T][n_splits][Hq] sum of the split's weights
   int* part_cls;        // [n_req][n_splits] widest class of the split's tiles, 0: none
 };
 
@@ -56,6 +66,14 @@ struct TreeCall {
 // queries, U_V^-1 (m_comps rows, 64 columns), the
 // scores (a tile's rows or sixteen of them, v_box columns).
 struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q, uv, scores, score_boxes; };
+
+// Two fp32 (packed) as three bf16 each: the nearest value, that of the rest, that of what is left then (24 bits in all).
+__device__ __forceinline__ void tree_split3(uint64_t v, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+  asm("{\n\t.reg .f32 a, b, c, d;\n\t.reg .b16 p, q, m;\n\tmov.b64 {a, b}, %3;\n\tmov.b16 m, 0xBF80;\n\t"
+      "cvt.rn.bf16x2.f32 %0, b, a;\n\tmov.b32 {p, q}, %0;\n\tfma.rn.f32.bf16 c, p, m, a;\n\tfma.rn.f32.bf16 d, q, m, b;\n\t"
+      "cvt.rn.bf16x2.f32 %1, d, c;\n\tmov.b32 {p, q}, %1;\n\tfma.rn.f32.bf16 a, p, m, c;\n\tfma.rn.f32.bf16 b, q, m, d;\n\t"
+      "cvt.rn.bf16x2.f32 %2, b, a;\n\t}" : "=&r"(hi), "=&r"(mid), "=r"(lo) : "l"(v));
+}
 
 // Rows of tree i; false where the offsets do not describe at most max_nodes rows of n_rows.
 __device__ __forceinline__ bool tree_rows(const int* offsets, int i, int n_rows, int max_nodes, int* first, int* n) {
@@ -77,7 +95,8 @@ cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, const TreeMap
 int tree_max_pairs(int sm_count);
 int tree_query_box(const TreeCall& a);
 int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count);
-int tree_merge_comps(int d_kv, int cl);
+int tree_merge_comps(int d_kv, int cl, int parts);
+int tree_value_range(int parts);
 cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);
 cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);
 

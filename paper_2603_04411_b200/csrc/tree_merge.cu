@@ -2,8 +2,8 @@
 //
 // A cluster of CL CTAs per (128 rows, KV head): row = (request, node; head of the group), and CTA c takes the spectral components
 // [c d/CL, (c + 1) d/CL), up to 128 at a time.  It sums their splits, each relative to its own maximum, normalises, and makes them the A operand of
-// a tcgen05 product with its rows of U_V^-1 (as they lie: MN-major B): two 16-bit parts of the cache type per component, fp32 accumulation in
-// tensor memory.  The CL partial products meet in distributed shared memory, 128 / CL columns per CTA.
+// a tcgen05 product with its rows of U_V^-1 (as they lie: MN-major B): two 16-bit parts of the cache type per component (three where a bf16 cache
+// has fp32 outputs), fp32 accumulation in tensor memory.  The CL partial products meet in distributed shared memory, 128 / CL columns per CTA.
 // What bounds it is the way of the partial sums (4 d_kv bytes per row and split) into the SMs, and for few rows the chain of reads, which a
 // cluster of eight shortens; with many rows the exchange would cost more than the rest (64 KiB per CTA of eight), so CL is the largest that leaves
 // two CTAs per SM.  The decode merge does the product by FMAs, which for hundreds of nodes cost several times the reads (256 nodes of 32
@@ -20,25 +20,27 @@ using namespace tc;
 
 constexpr int TM_THREADS = 256;
 constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 components] of one part
-constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // high and low parts of up to 128 components; their rows of U_V^-1, 128 columns
+constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // two parts of up to 128 components (three of 64); their rows of U_V^-1, 128 columns
 constexpr int TM_FEW = 4;                                     // splits whose weights are looked up once per row
-constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16 + TM_FEW * 3 * 4 + TM_FEW) + 64;
+constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16 + TM_FEW * TREE_MAX_RANGES * 4 + TM_FEW) + 64;
 static_assert(2 * TM_SMEM <= 228 * 1024 - 2 * 1024, "two CTAs per SM");
+static_assert(TREE_MAX_SPLITS <= 64, "two splits per lane");
 static_assert(TILE * HEAD_DIM * 4 <= TM_A, "the partial products arrive where the A operand was");
 
 __device__ __forceinline__ float tm_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
-template <bool BF16, int CL>
+template <bool BF16, int PARTS, int CL>
 __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
   float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE, *s_w = s_inv + TILE;      // per row
-  int4* s_row = reinterpret_cast<int4*>(s_w + TILE * TM_FEW * 3);                     // first part, splits, request, row of the outputs; -1: none
+  int4* s_row = reinterpret_cast<int4*>(s_w + TILE * TM_FEW * TREE_MAX_RANGES);                     // first part, splits, request, row of the outputs; -1: none
   unsigned char* s_cls = reinterpret_cast<unsigned char*>(s_row + TILE);
   unsigned char* tail = s_cls + TILE * TM_FEW;
   const uint32_t b_full = smem_addr(tail), done = b_full + 8;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(tail + 16);
   volatile int* abort_flag = reinterpret_cast<int*>(s_tmem + 1);
+  constexpr uint32_t PART = PARTS == 3 ? TM_PANEL : 2 * TM_PANEL;                     // bytes of one part of the A operand
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int c = CL > 1 ? (int)cluster_cta_rank() : 0, g = blockIdx.y, rep = v.rep, jn = a.m_comps;      // components at a time: a multiple of 16, at most 128
   const int slot0 = (blockIdx.x / CL) * (TILE / rep), n_slots = a.n_req * a.T;
@@ -68,30 +70,36 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     if (slot < n_slots && t < info.y) {
       used = info.w;                                            // splits that hold something come first
       row = slot * a.n_splits * v.Hq + g * rep + tid % rep;
-      const float4* ml = a.part_ml + row;
+      const float4* refs = a.part_m + row;
+      const float* sums = a.part_l + row;
       for (int s0 = 0; s0 < used; s0 += 4) {
         float4 y[4];
+        float l[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) y[k] = s0 + k < used ? ml[(size_t)(s0 + k) * v.Hq] : make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        for (int k = 0; k < 4; ++k) {
+          y[k] = s0 + k < used ? refs[(size_t)(s0 + k) * v.Hq] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+          l[k] = s0 + k < used ? sums[(size_t)(s0 + k) * v.Hq] : 0.f;
+        }
         const float m = fmaxf(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), most);
         sum *= most == -INFINITY ? 0.f : tm_ex2(most - m);      // (one that is not a number stays one)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) sum += y[k].w * (y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m));
+        for (int k = 0; k < 4; ++k) sum += l[k] * (y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m));
         most = m;
         if (used <= TM_FEW) {
 #pragma unroll
           for (int k = 0; k < TM_FEW; ++k) {
             s_cls[tid * TM_FEW + k] = k < used ? (unsigned char)a.part_cls[req * a.n_splits + k] : 0;
-            const float ref[3] = {y[k].x, y[k].y, y[k].z};
+            const float ref[TREE_MAX_RANGES] = {y[k].x, y[k].y, y[k].z, y[k].w};
 #pragma unroll
-            for (int e = 0; e < 3; ++e) s_w[(tid * TM_FEW + k) * 3 + e] = ref[e] == -INFINITY ? 0.f : tm_ex2(ref[e] - m);
+            for (int e = 0; e < TREE_MAX_RANGES; ++e) s_w[(tid * TM_FEW + k) * TREE_MAX_RANGES + e] = ref[e] == -INFINITY ? 0.f : tm_ex2(ref[e] - m);
           }
         }
       }
     }
     s_row[tid] = make_int4(row, used, req, slot < n_slots && t < info.y ? info.x + t : -1);
     s_most[tid] = most;
-    s_inv[tid] = sum == 0.f ? 0.f : 1.f / sum;                  // 0: no token seen
+    // 0: no token seen.  (With what the products' sum is expected to lose.)
+    s_inv[tid] = sum == 0.f ? 0.f : (1.f + TREE_CUT * (float)(v.d_kv / CL / 16 * PARTS)) / sum;
   }
   __syncthreads();
   // Sums: a warp takes rows warp, warp + 8, ..., its lanes four components.  Eight reads on their way: of as many rows where a row has few splits, of
@@ -100,22 +108,24 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   auto put = [&](int r, float4 x) {                             // a row's normalised components as the A operand
     if (!mine) return;
     const float il = s_inv[r];
-    uint32_t hi[2], lo[2];
-    uint64_t w;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.x * il), "f"(x.y * il));
-    split_pair_16<BF16>(w, hi[0], lo[0]);
-    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(x.z * il), "f"(x.w * il));
-    split_pair_16<BF16>(w, hi[1], lo[1]);
+    uint32_t w[PARTS][2];                                       // the largest part first
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint64_t y;
+      asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"((h ? x.z : x.x) * il), "f"((h ? x.w : x.y) * il));
+      if constexpr (PARTS == 3) tree_split3(y, w[0][h], w[1][h], w[2][h]);
+      else split_pair_16<BF16>(y, w[0][h], w[1][h]);
+    }
     const int e = lane * 4;
-    unsigned char* d = smem + (e >> 6) * TM_PANEL + r * 128 + ((((e >> 3) & 7) ^ (r & 7)) << 4) + (e & 7) * 2;
-    *reinterpret_cast<uint2*>(d) = make_uint2(hi[0], hi[1]);
-    *reinterpret_cast<uint2*>(d + 2 * TM_PANEL) = make_uint2(lo[0], lo[1]);
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p)
+      *reinterpret_cast<uint2*>(smem + p * PART + (e >> 6) * TM_PANEL + r * 128 + ((((e >> 3) & 7) ^ (r & 7)) << 4) + (e & 7) * 2) = make_uint2(w[p][0], w[p][1]);
   };
   bool ok = !misaligned;
   uint32_t ph = 0;
   const int first = c * (v.d_kv / CL), n_chunks = v.d_kv / CL / jn;
   for (int chunk = 0; chunk < n_chunks; ++chunk) {
-    const int j0 = first + chunk * jn, comp = j0 + lane * 4, range = comp / (TREE_RANGE * PANEL);
+    const int j0 = first + chunk * jn, comp = j0 + lane * 4, range = comp / (a.range * PANEL);
     if (warp == 0 && elect_one() && ok) {                      // U_V^-1, on its way while the splits are summed
       mbar_expect_tx(b_full, (uint32_t)jn * 256u);
       tma_load_2d(sB, &map_uv, b_full, g * HEAD_DIM, j0);
@@ -144,7 +154,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
             const int r = warp + 8 * (b + k);
             const int4 q = s_row[r];
             const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
-            const float w = in ? s_w[(r * TM_FEW + s) * 3 + range] : 0.f;
+            const float w = in ? s_w[(r * TM_FEW + s) * TREE_MAX_RANGES + range] : 0.f;
             x[k].x += y[k].x * w; x[k].y += y[k].y * w; x[k].z += y[k].z * w; x[k].w += y[k].w * w;
           }
         }
@@ -157,7 +167,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
         const int4 q = s_row[r];
         if (q.x < 0) continue;
         const int* cls = a.part_cls + q.z * a.n_splits;
-        const float* refs = reinterpret_cast<const float*>(a.part_ml + q.x) + range;
+        const float* refs = reinterpret_cast<const float*>(a.part_m + q.x) + range;
         const float most = s_most[r];
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
@@ -186,11 +196,11 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
         fence_after_sync();
         constexpr uint32_t idesc = idesc_f16(BF16 ? 1 : 0, 128, 128) | (1u << 16);       // B MN-major
         const uint32_t b_lo = ((sB >> 4) & 0x3fffu) | ((uint32_t)(jn * 128) >> 4 << 16);
-        for (int part = 1; part >= 0; --part)                     // the low parts first: the sum is cut after every instruction
+        for (int part = PARTS - 1; part >= 0; --part)                     // the low parts first: the sum is cut after every instruction
           for (int ks = 0; ks < jn / 16; ++ks) {
-            const uint32_t a_lo = kmajor_sw128_desc_lo(sA + part * 2 * TM_PANEL + (ks >> 2) * TM_PANEL) + 2 * (ks & 3);
+            const uint32_t a_lo = kmajor_sw128_desc_lo(sA + part * PART + (ks >> 2) * TM_PANEL) + 2 * (ks & 3);
             mma_f16_ss(tmem, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | a_lo, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u), idesc,
-                       chunk > 0 || part == 0 || ks > 0 ? 1u : 0u);
+                       chunk > 0 || part < PARTS - 1 || ks > 0 ? 1u : 0u);
           }
         mma_commit(done);
       }
@@ -278,32 +288,33 @@ int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count) {
   while (cl > 1 && work * cl > 2 * sm_count) cl /= 2;
   return cl;
 }
-// Components that a CTA takes at a time: the least number of equal pieces of at most 128, a multiple of sixteen each.
-int tree_merge_comps(int d_kv, int cl) {
-  int n = (d_kv / cl + 127) / 128;
+// Components that a CTA takes at a time: the least number of equal pieces of at most 128 (three parts: 64), a multiple of sixteen each.
+int tree_merge_comps(int d_kv, int cl, int parts) {
+  const int most = parts == 3 ? 64 : 128;
+  int n = (d_kv / cl + most - 1) / most;
   while (d_kv / cl % (16 * n)) ++n;
   return d_kv / cl / n;
 }
 
-template <bool BF16, int CL>
+template <bool BF16, int PARTS, int CL>
 static cudaError_t launch_tree_merge_t(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(tree_merge_kernel<BF16, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TM_SMEM);
+  cudaError_t e = cudaFuncSetAttribute(tree_merge_kernel<BF16, PARTS, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TM_SMEM);
   if (e != cudaSuccess) return e;
   const int tiles = (a.n_req * a.T * v.rep + TILE - 1) / TILE;
-  return launch_chained(tree_merge_kernel<BF16, CL>, dim3(CL * tiles, v.Hkv), dim3(TM_THREADS), dim3(CL), TM_SMEM, st, maps.uv, v, a);
+  return launch_chained(tree_merge_kernel<BF16, PARTS, CL>, dim3(CL * tiles, v.Hkv), dim3(TM_THREADS), dim3(CL), TM_SMEM, st, maps.uv, v, a);
 }
-template <bool BF16>
+template <bool BF16, int PARTS>
 static cudaError_t launch_tree_merge_cl(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
   switch (a.m_cluster) {
-    case 1: return launch_tree_merge_t<BF16, 1>(v, a, maps, st);
-    case 2: return launch_tree_merge_t<BF16, 2>(v, a, maps, st);
-    case 4: return launch_tree_merge_t<BF16, 4>(v, a, maps, st);
-    default: return launch_tree_merge_t<BF16, 8>(v, a, maps, st);
+    case 1: return launch_tree_merge_t<BF16, PARTS, 1>(v, a, maps, st);
+    case 2: return launch_tree_merge_t<BF16, PARTS, 2>(v, a, maps, st);
+    case 4: return launch_tree_merge_t<BF16, PARTS, 4>(v, a, maps, st);
+    default: return launch_tree_merge_t<BF16, PARTS, 8>(v, a, maps, st);
   }
 }
 cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
   ProfScope ps(TWKV_K_MERGE, st);
-  const cudaError_t e = v.dtype == TWKV_BF16 ? launch_tree_merge_cl<true>(v, a, maps, st) : launch_tree_merge_cl<false>(v, a, maps, st);
+  const cudaError_t e = v.dtype != TWKV_BF16 ? launch_tree_merge_cl<false, 2>(v, a, maps, st) : a.n_parts == 3 ? launch_tree_merge_cl<true, 3>(v, a, maps, st) : launch_tree_merge_cl<true, 2>(v, a, maps, st);
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaGetLastError();

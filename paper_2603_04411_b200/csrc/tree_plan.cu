@@ -280,8 +280,8 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
       m = make_int4(i * (v.TPS + 1) + nv, r.w >> 8, r.y, -1);
     }
     meta[k] = m;
-    // in panels' products: a tile's weights take as long as those of four panels; wide tiles are taken in ranges of six, by CTAs of their own
-    return vtile_boxes(m.z) * max(min(m.y, TREE_RANGE), 4) + 4;
+    // in panels' products: a tile's weights take as long as those of four panels; wide tiles are taken in ranges, by CTAs of their own
+    return vtile_boxes(m.z) * max(min(m.y, a.range), 4) + 4;
   };
   int total = 0;
   for (int k0 = 0; k0 < n; k0 += 1024) {

@@ -340,7 +340,9 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     uint32_t sbuf = 0, sph = 0;
     bool ok = true;
     uint64_t cs2[16], sn2[16];                                    // the tile's rotation factors, frequencies (2 t, 2 t + 1) packed
-    auto rope_setup = [&](int pos) {
+    auto rope_setup = [&](int2 at) {                               // position, class of the row
+      const int pos = at.x, chain = 4 * min(at.y, panels(at.y));   // instructions that a key of the row was summed in
+      const uint64_t up = ts_pack(1.f + TREE_CUT * (float)chain, 1.f + TREE_CUT * (float)chain);
       const float4* __restrict__ th = rope_hi + (size_t)((pos >> 4) & (ROPE_HI - 1)) * 32 + hf * 16;
       const float4* tl = sRope + (pos & 15) * TS_ROPE_STRIDE + hf * 16;
       float4 h[16];
@@ -350,23 +352,28 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
       for (int t = 0; t < 16; ++t) {
         const float4 l = tl[t];
         const uint64_t ch = ts_pack(h[t].x, h[t].y), sh = ts_pack(h[t].z, h[t].w), cl = ts_pack(l.x, l.y), sl = ts_pack(l.z, l.w);
-        cs2[t] = ts_sub(ts_mul(ch, cl), ts_mul(sh, sl));
-        sn2[t] = ts_fma(sh, cl, ts_mul(ch, sl));
+        cs2[t] = ts_mul(ts_sub(ts_mul(ch, cl), ts_mul(sh, sl)), up);
+        sn2[t] = ts_mul(ts_fma(sh, cl, ts_mul(ch, sl)), up);
       }
     };
-    auto row_pos = [&](const int4& e) -> int {
-      if (cached(e)) return e.x < 0 ? v.joint_pos()[(size_t)~e.x * TILE + row] : kpos[(size_t)e.x * TILE + row];
-      if (e.w >= 0 && (e.y & TREE_NODES) && row < (e.y >> 16)) return a.positions[a.info[e.w].x + row];
-      return 0;
+    auto row_at = [&](const int4& e) -> int2 {
+      const int cls = e.y & TREE_CLASS;
+      if (cached(e) && e.x < 0) {
+        const int k = v.joint_rows()[(size_t)~e.x * TILE + row];
+        return make_int2(v.joint_pos()[(size_t)~e.x * TILE + row], k >= 0 ? v.desc(layer, 0)[k / TILE].y : cls);
+      }
+      if (cached(e)) return make_int2(kpos[(size_t)e.x * TILE + row], cls);
+      if (e.w >= 0 && (e.y & TREE_NODES) && row < (e.y >> 16)) return make_int2(a.positions[a.info[e.w].x + row], cls);
+      return make_int2(0, cls);
     };
     TsUnit u = unit(w0);
-    if (w0 < total) rope_setup(row_pos(u.e));
+    if (w0 < total) rope_setup(row_at(u.e));
     for (int w = w0; w < total && ok; ++w) {
       const TsUnit nxt = unit(w + 1);
       [[maybe_unused]] bool has_row = true;
       if constexpr (DBG) has_row = cached(u.e) ? cache_slot(u.e, row) >= 0 : (u.e.y & TREE_NODES) && row < (u.e.y >> 16);
       const int passes = u.cls > panels(u.cls) ? 2 : 1;
-      const int pos_next = row_pos(nxt.e);                                        // fetched now, used after the tile's slabs
+      const int2 at_next = row_at(nxt.e);                                         // fetched now, used after the tile's slabs
       for (int ps = 0; ps < passes && ok; ++ps) {
         for (int sli = 0; sli < nh; ++sli) {
           if (!(ok = __all_sync(0xffffffffu, mbar_wait(slab_full + 8 * sbuf, sph, abort_flag)))) break;
@@ -411,7 +418,7 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         }
       }
       if (!ok) break;
-      if (nxt.e.w >= 0 && (nxt.e.x != u.e.x || nxt.e.y != u.e.y)) rope_setup(pos_next);      // a further part of the same tile: the factors stay
+      if (nxt.e.w >= 0 && (nxt.e.x != u.e.x || nxt.e.y != u.e.y)) rope_setup(at_next);      // a further part of the same tile: the factors stay
       u = nxt;
     }
     tmem_ld_wait();                                                          // nothing of this thread is in flight when TMEM is freed

@@ -4,10 +4,10 @@
 //   acc[c][j] = sum over the split's tokens t of p[t][c] X^_V[t][j],   p = exp(s - top[c]),   l[c] = sum of p[t][c]
 // The weights are the A operand, from tensor memory (M = 128 query rows, K = 16 tokens per instruction), and the panels of a V tile, as TMA lands
 // them, the MN-major B operand (N = 128: two panels): a panel is read from shared memory once per 128 rows and part of the weights, which
-// come as two parts of the cache type.  (With the panels as A and 64 columns of weights as B, both from shared memory, an instruction of half the
+// come as two parts of the cache type, or three where bf16 caches have fp32 outputs.  (With the panels as A and 64 columns of weights as B, both from shared memory, an instruction of half the
 // work took 85 cycles for its operands instead of 32: 12200 cycles per tile of sixteen panels and 64 columns.)
-// Tensor memory holds the weights of one tile (128 columns: 64 of high parts, 64 of low ones) and three accumulators of 128 columns: six panels.  A
-// CTA therefore takes a range of six panels (blockIdx.z); the wider ranges, which only wide tiles reach, form those tiles' weights again.
+// Tensor memory holds the weights of one tile (64 columns per part) and three accumulators of 128 columns: six panels (with three parts two: four).  A
+// CTA therefore takes a range of six panels (blockIdx.z); the higher ranges, which only wide tiles reach, form those tiles' weights again.
 // A tile's scores come by TMA while the tile before is worked on (read from memory by the lanes themselves, whose registers hold one tile, their
 // latency bound the kernel: 5600 cycles per narrow tile).  What a row's weights are relative to, top[c],
 // is its largest score so far, moved only when it would grow by more than 2^8 (f16 holds 2^15): the accumulators are rescaled seldom, by the
@@ -29,11 +29,9 @@ constexpr int TV_REGS_LIGHT = 64, TV_REGS_WEIGHTS = 104;       // 128 x 64 + 512
 constexpr int TV_META = 256;                                   // tiles whose descriptors are staged in shared memory at a time
 constexpr int TV_STAGES = 4;
 constexpr uint32_t TV_PANEL = 16384, TV_STAGE = 2 * TV_PANEL;
-constexpr uint32_t TV_COL_P = 384;                             // behind three accumulators
 constexpr uint32_t TV_SCORES = TILE * TILE * 4;                 // a tile's scores with 128 query rows
 constexpr uint32_t TV_SMEM = TV_STAGES * TV_STAGE + TV_SCORES + TV_META * 16 + 2 * 4 * TILE * 4 + 256;
 static_assert(TV_SMEM > CHAIN_TMEM_SMEM && TV_SMEM <= 232448, "no other CTA with tensor memory beside this one");
-static_assert(TREE_RANGE == 6, "three accumulators of two panels");
 static_assert(2 * TREE_PANEL_ROWS <= TILE, "the nodes' tile always comes in boxes");
 
 constexpr float TV_LOG2E = 1.44269504088896340736f;
@@ -43,14 +41,31 @@ __device__ __forceinline__ uint64_t tv_fma2(uint64_t a, uint64_t b, uint64_t c) 
 __device__ __forceinline__ uint64_t tv_add2(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
 __device__ __forceinline__ float tv_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 
-template <bool BF16>
+// PARTS = 2: three accumulators of two panels, then the weights (2 x 64 columns); 3: two accumulators and 3 x 64 columns.
+__host__ __device__ constexpr int tv_range(int parts) { return parts == 3 ? 4 : 6; }
+int tree_value_range(int parts) { return tv_range(parts); }
+static_assert((TWKV_MAX_CLASSES + tv_range(3) - 1) / tv_range(3) <= TREE_MAX_RANGES, "a reference per range");
+static_assert(tv_range(2) * 64 + 2 * 64 <= 512 && tv_range(3) * 64 + 3 * 64 <= 512, "tensor memory");
+
+__device__ __forceinline__ void tv_ld8(const float* p, float* x) {
+  asm volatile("ld.global.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7]) : "l"(__cvta_generic_to_global(p)) : "memory");
+}
+__device__ __forceinline__ void tv_st8(float* p, const float* x) {
+  asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(__cvta_generic_to_global(p)), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]) : "memory");
+}
+
+template <bool BF16, int PARTS>
 __global__ void __launch_bounds__(TV_THREADS, 1)
 tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_constant__ CUtensorMap map_boxes, const __grid_constant__ CUtensorMap map_nodes,
                   const __grid_constant__ CUtensorMap map_scores, const __grid_constant__ CUtensorMap map_score_boxes, DevView v, TreeCall a) {
+  constexpr int RANGE = tv_range(PARTS), COLS = RANGE * PANEL;
+  constexpr uint32_t COL_P = COLS;
   chain_start();
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int req = blockIdx.x / a.n_splits, split = blockIdx.x - req * a.n_splits, c0 = blockIdx.y * TILE, range = blockIdx.z, panel0 = range * TREE_RANGE;
+  const int req = blockIdx.x / a.n_splits, split = blockIdx.x - req * a.n_splits, c0 = blockIdx.y * TILE, range = blockIdx.z, panel0 = range * RANGE;
   // shared memory: ring | scores [128 tokens][columns of a box] | descriptors | maxima [2][4 parts][128 rows] | barriers
   const uint32_t sRing = smem_addr(smem_raw);
   const bool misaligned = (sRing & 1023u) != 0;                 // operand tiles need 1024-byte alignment for the swizzle
@@ -92,6 +107,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TV_REGS_LIGHT));
     uint32_t st = 0, st_ph = 0, n_loaded = 0;                   // ring stage and its phase; stages filled so far
+    int since = 0;                                              // tiles in the accumulators
     for (int k0 = 0; k0 < n_mine; k0 += TV_META) {
       if (warp == 0) {
         // the chunk's tiles that reach the range, in order
@@ -118,7 +134,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
           if (k0 == 0) { tma_prefetch_desc(&map_blocks); tma_prefetch_desc(&map_boxes); tma_prefetch_desc(&map_nodes); }
           for (int i = 0; i < cn && ok; ++i) {
             const int4 m = s_meta[i];
-            const int nb = vtile_boxes(m.z), end = min(m.y, panel0 + TREE_RANGE);
+            const int nb = vtile_boxes(m.z), end = min(m.y, panel0 + RANGE);
             for (int j = panel0; j < end; j += 2) {
               if (!(ok = mbar_wait_thin(empty + 8 * st, st_ph ^ 1u, abort_flag))) break;
               // (a lone panel is followed by zeros from behind the last block: the accumulator's other half has to hold something)
@@ -150,28 +166,33 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         if (elect_one()) {
           for (int i = 0; i < cn && ok; ++i, ++k) {
             const int4 m = s_meta[i];
-            const int nb = vtile_boxes(m.z), end = min(m.y, panel0 + TREE_RANGE);
+            const int nb = vtile_boxes(m.z), end = min(m.y, panel0 + RANGE);
             if (!(ok = mbar_wait_thin(p_full, k & 1u, abort_flag))) break;
             fence_after_sync();
+            if (since == a.drain) { touched = 0; since = 0; }      // the weight warps have emptied the accumulators
+            ++since;
             for (int j = panel0; j < end; j += 2) {
               if (!(ok = mbar_wait_thin(full + 8 * st, st_ph, abort_flag))) break;
               fence_after_sync();
-              const uint32_t acc = (uint32_t)(j - panel0) >> 1, d = tmem_base + acc * 128, w = tmem_base + TV_COL_P;
+              const uint32_t acc = (uint32_t)(j - panel0) >> 1, d = tmem_base + acc * 128, w = tmem_base + COL_P;
               constexpr uint32_t idesc = idesc_f16(BF16 ? 1 : 0, 128, 128) | (1u << 16);            // B MN-major
               const uint32_t b_lo = (((sRing + st * TV_STAGE) >> 4) & 0x3fffu) | ((TV_PANEL >> 4) << 16);
               uint32_t more = (touched >> acc) & 1u;
-              auto step = [&](int ks) {                           // 16 tokens; the low parts of their weights first
-                const uint64_t b = ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u);
-                mma_f16_ts(d, w + 64 + 8 * ks, b, idesc, more);
-                mma_f16_ts(d, w + 8 * ks, b, idesc, 1u);
+              auto step = [&](int p, int ks) {                  // one part of the weights of 16 tokens
+                mma_f16_ts(d, w + 64 * p + 8 * ks, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u), idesc, more);
                 more = 1u;
               };
+              // the small parts of all tokens first: the sum is cut after every instruction
               if (nb == TILE / JOINT_ROWS) {                      // (a loop of its own: the checks would cost this thread its pace)
 #pragma unroll
-                for (int ks = 0; ks < 8; ++ks) step(ks);
+                for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+                  for (int ks = 0; ks < 8; ++ks) step(p, ks);
               } else {
 #pragma unroll 1
-                for (int ks = 0; ks < nb; ++ks) step(ks);
+                for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll 1
+                  for (int ks = 0; ks < nb; ++ks) step(p, ks);
               }
               touched |= 1u << acc;
               mma_commit(empty + 8 * st);
@@ -209,6 +230,41 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     const float scale = (v.sm_scale == 0.f ? 1.f : fabsf(v.sm_scale)) * TV_LOG2E;      // scores come without their scale; weights are powers of two
     const uint64_t scale2 = tv_pack(scale, scale);
     const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    // Row of the partial results that this thread's column of the request stands for; -1: no node's.
+    const int c = c0 + row, g = c / a.Rs, n = c - g * a.Rs, t = n / v.rep;
+    const long long r = c < a.C && n < a.R && t < info.y ? ((long long)(req * a.T + t) * a.n_splits + split) * v.Hq + g * v.rep + n % v.rep : -1;
+    // The tensor core cuts its fp32 sums after every instruction, so an accumulator's error grows with the tiles in it.  After `drain` tiles it is emptied,
+    // its expected loss given back, onto the partial result in memory: `stored`, accumulators that have been; worth `kept` of what it was then.
+    float* const out = a.part_acc + (size_t)(r < 0 ? 0 : r) * v.d_kv + panel0 * PANEL;
+    const int col0 = part * (COLS / 4);
+    uint32_t stored = 0;
+    int since = 0, chain[RANGE / 2] = {};                         // tiles, and instructions, in the accumulators
+    float kept = 1.f;
+    auto read_out = [&](int c, float (&o)[32]) {                 // 32 of this thread's columns of the partial result
+#pragma unroll
+      for (int b = 0; b < 32; b += 8)
+        if (r >= 0 && ((stored >> ((c + b) >> 7)) & 1u)) tv_ld8(out + c + b, o + b);
+    };
+    auto empty_onto = [&](int c, float (&o)[32], float f) {       // and the accumulators' columns, times f, onto them
+#pragma unroll
+      for (int b = 0; b < 32; b += 8) {
+        const uint32_t acc = (uint32_t)(c + b) >> 7;
+        const bool held = (stored >> acc) & 1u, fresh = (touched >> acc) & 1u;
+        if (!held && !fresh) continue;
+        float fc = f;
+#pragma unroll
+        for (int e = 0; e < RANGE / 2; ++e)
+          if (acc == (uint32_t)e) fc = f * (1.f + TREE_CUT * (float)chain[e]);
+        float d[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (fresh) {
+          tmem_ld8(lanes + c + b, reinterpret_cast<uint32_t*>(d));
+          tmem_ld_wait();
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] = held ? o[b + e] * kept + d[e] * fc : d[e] * fc;
+        if (r >= 0) tv_st8(out + c + b, d);
+      }
+    };
     float top = -INFINITY;
     uint64_t l_sum2 = 0;                                        // two sums of this thread's weights
     for (int k0 = 0; k0 < n_mine; k0 += TV_META) {
@@ -251,23 +307,41 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         float la, lb;
         tv_unpack(l_sum2, la, lb);
         l_sum2 = tv_pack(la * f, lb * f);
+        kept *= f;
         const bool any = part * 32 < vtile_boxes(m.z) * JOINT_ROWS;      // (the products leave the other tokens out)
-        uint32_t hi[16], lo[16];
+        uint32_t w[PARTS][16];                                    // the largest part first
 #pragma unroll
         for (int u = 0; u < 32; u += 2) {
           float x0, x1;
           tv_unpack(tv_fma2(tv_pack(x[u], x[u + 1]), scale2, nm2), x0, x1);
           const uint64_t p = tv_pack(tv_ex2(x0), tv_ex2(x1));
           l_sum2 = tv_add2(l_sum2, p);
-          split_pair_16<BF16>(p, hi[u >> 1], lo[u >> 1]);
+          if constexpr (PARTS == 3) tree_split3(p, w[0][u >> 1], w[1][u >> 1], w[2][u >> 1]);
+          else split_pair_16<BF16>(p, w[0][u >> 1], w[1][u >> 1]);
         }
         if (k > 0) {
+          const bool full_up = since == a.drain;
+          float o[32];
+          if (full_up) read_out(col0, o);
           ok = __all_sync(0xffffffffu, mbar_wait(p_done, (k - 1) & 1u, abort_flag));
           fence_after_sync();
-          if (__any_sync(0xffffffffu, grow) && ok) {
+          if (full_up && ok) {
+            empty_onto(col0, o, f);
+#pragma unroll 1
+            for (int c = col0 + 32; c < col0 + COLS / 4; c += 32) {
+              read_out(c, o);
+              empty_onto(c, o, f);
+            }
+            stored |= touched;
+            touched = 0;
+            since = 0;
+            kept = 1.f;
+#pragma unroll
+            for (int e = 0; e < RANGE / 2; ++e) chain[e] = 0;
+          } else if (__any_sync(0xffffffffu, grow) && ok) {
             // seldom: this part's columns of the accumulators take the rows' factors
 #pragma unroll 1
-            for (int c = part * 96; c < part * 96 + 96; c += 8) {
+            for (int c = col0; c < col0 + COLS / 4; c += 8) {
               if (!((touched >> (c >> 7)) & 1u)) continue;
               uint32_t o[8];
               tmem_ld8(lanes + c, o);
@@ -278,11 +352,16 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
             }
           }
         }
+        ++since;
         if (!ok) continue;
-        touched |= (1u << ((min(m.y, panel0 + TREE_RANGE) - panel0 + 1) >> 1)) - 1u;
+        const int reach = (min(m.y, panel0 + RANGE) - panel0 + 1) >> 1;
+#pragma unroll
+        for (int e = 0; e < RANGE / 2; ++e)                       // (the small parts of an accumulator's first tile come before its sum has its size)
+          if (e < reach) chain[e] += vtile_boxes(m.z) * ((touched >> e) & 1u ? PARTS : 1);
+        touched |= (1u << reach) - 1u;
         if (any) {
-          tmem_st16(lanes + TV_COL_P + 16 * part, hi);
-          tmem_st16(lanes + TV_COL_P + 64 + 16 * part, lo);
+#pragma unroll
+          for (int p = 0; p < PARTS; ++p) tmem_st16(lanes + COL_P + 64 * p + 16 * part, w[p]);
         }
         tmem_st_wait();
         fence_before_sync();
@@ -293,35 +372,25 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
       ok = ok && !*abort_flag;
     }
     // ----------------------------------------------------------- partial results of this split
-    // Row of the partial results that this thread's column of the request stands for; -1: no node's.
-    const int c = c0 + row, g = c / a.Rs, n = c - g * a.Rs, t = n / v.rep;
-    const long long r = c < a.C && n < a.R && t < info.y ? ((long long)(req * a.T + t) * a.n_splits + split) * v.Hq + g * v.rep + n % v.rep : -1;
     float la, lb;
     tv_unpack(l_sum2, la, lb);
     s_max[part * TILE + row] = la + lb;                         // (behind the loop's last __syncthreads: nobody reads maxima any more)
     if (ok && k > 0) ok = __all_sync(0xffffffffu, mbar_wait(p_done, (k - 1) & 1u, abort_flag));
     fence_after_sync();
     named_bar_sync(1 + quarter, 128);
-    // This part's 96 columns, a row per thread; columns that no tile reached are left alone, as is everything where no tile reached the range: the
+    // This part's columns, a row per thread; columns that no tile reached are left alone, as is everything where no tile reached the range: the
     // merge knows it from the split's widest class.
-    float* const out = a.part_acc + (size_t)(r < 0 ? 0 : r) * v.d_kv + panel0 * PANEL;
-    const int end = ok && k > 0 ? min(s_count[1] - panel0, TREE_RANGE) * PANEL : 0;
+    if (ok && k > 0) {
 #pragma unroll 1
-    for (int e = part * 96; e < part * 96 + 96; e += 32) {
-      if (e >= end) break;
-      uint32_t x[32];
-      tmem_ld32(lanes + e, x);
-      tmem_ld_wait();
-      if (r < 0) continue;
-#pragma unroll
-      for (int b = 0; b < 32; b += 8)
-        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(out + e + b)), "r"(x[b]), "r"(x[b + 1]),
-                     "r"(x[b + 2]), "r"(x[b + 3]), "r"(x[b + 4]), "r"(x[b + 5]), "r"(x[b + 6]), "r"(x[b + 7]) : "memory");
+      for (int c = col0; c < col0 + COLS / 4; c += 32) {
+        float o[32];
+        read_out(c, o);
+        empty_onto(c, o, 1.f);
+      }
     }
     if (part == 0 && r >= 0) {
-      float* const ml = reinterpret_cast<float*>(a.part_ml + r);
-      ml[range] = top;
-      if (range == 0) ml[3] = (s_max[row] + s_max[TILE + row]) + (s_max[2 * TILE + row] + s_max[3 * TILE + row]);
+      reinterpret_cast<float*>(a.part_m + r)[range] = top;
+      if (range == 0) a.part_l[r] = (s_max[row] + s_max[TILE + row]) + (s_max[2 * TILE + row] + s_max[3 * TILE + row]);
     }
     tmem_ld_wait();
   }
@@ -335,10 +404,10 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
 
 cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
   ProfScope ps(TWKV_K_VACC, st);
-  auto kernel = v.dtype == TWKV_BF16 ? tree_value_kernel<true> : tree_value_kernel<false>;
+  auto kernel = v.dtype != TWKV_BF16 ? tree_value_kernel<false, 2> : a.n_parts == 3 ? tree_value_kernel<true, 3> : tree_value_kernel<true, 2>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TV_SMEM);
   if (e != cudaSuccess) return e;
-  e = launch_chained(kernel, dim3(a.n_req * a.n_splits, (a.C + TILE - 1) / TILE, (v.NC + TREE_RANGE - 1) / TREE_RANGE), dim3(TV_THREADS), dim3(1), TV_SMEM, st,
+  e = launch_chained(kernel, dim3(a.n_req * a.n_splits, (a.C + TILE - 1) / TILE, (v.NC + a.range - 1) / a.range), dim3(TV_THREADS), dim3(1), TV_SMEM, st,
                      maps.blocks, maps.boxes, maps.node_boxes, maps.scores, maps.score_boxes, v, a);
   if (e != cudaSuccess) return e;
   count_launch();
