@@ -958,14 +958,14 @@ twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* 
     a.q = (const unsigned short*)q; a.K = (const unsigned short*)K; a.V = (const unsigned short*)V; a.levels = levels;
     a.req_seqs = req_seqs; a.offsets = offsets; a.positions = positions; a.masks = (const unsigned long long*)masks;
     a.out = out; a.n_rows = n_rows; a.r0 = r0;
-    if (launch_tree_plan(c->view, a, layer, n_pieces, st) != cudaSuccess) return TWKV_ERR_CUDA;
+    if (launch_tree_plan(c->view, a, layer, n_pieces, c->sm_count, st) != cudaSuccess) return TWKV_ERR_CUDA;
     TreeMaps maps;
     maps.blocks = c->map_blocks;
     maps.boxes = c->map_boxes;
     const uint64_t node_rows = (uint64_t)a.n_req * v.NC * TREE_PANEL_ROWS;
     a.q_box = tree_query_box(a);
     a.v_box = std::min(a.C, TILE);
-    a.m_cluster = tree_merge_cluster(v, a, c->sm_count);
+    a.m_cluster = tree_merge_cluster(v, a, c->sm_count, &a.m_rows);
     a.m_comps = tree_merge_comps(v.d_kv, a.m_cluster, a.n_parts);
     const uint64_t score_rows = (uint64_t)a.n_req * (v.TPS + 1) * TILE;
     if (!make_tmap_2d_f32(&maps.scores, a.scores, score_rows, (uint64_t)a.C, TILE, (uint32_t)a.v_box) ||

@@ -40,7 +40,7 @@ struct TreeCall {
   int n_splits;
   int entries;          // room of a request in the K list
   int q_box;            // rows of qop that a CTA takes at a time
-  int m_cluster, m_comps;     // CTAs of a cluster of the merge, components that each takes at a time
+  int m_cluster, m_rows, m_comps;     // CTAs of a cluster of the merge, query rows of a cluster, components that each CTA takes at a time
   int n_parts;          // parts that a weight, and a component of the merge, goes into products as
   int drain;            // tiles that an accumulator of the value kernel takes before it is emptied
   int range;            // panels whose sums a CTA of the value kernel keeps
@@ -90,11 +90,11 @@ cudaError_t launch_tree_map(const DevView& v, const int* offsets, const int* par
                             unsigned long long* masks, cudaStream_t st);
 cudaError_t launch_tree_accept(const DevView& v, const int* offsets, const int* parents, const int* draft, const int* target, int n_req, int n_rows,
                                int max_nodes, int* n_accepted, int* rows, int* next_tokens, cudaStream_t st);
-cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int n_pieces, cudaStream_t st);
+cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int n_pieces, int sm_count, cudaStream_t st);
 cudaError_t launch_tree_score(const DevView& v, const TreeCall& a, const TreeMaps& maps, int layer, int n_pieces, cudaStream_t st);
 int tree_max_pairs(int sm_count);
 int tree_query_box(const TreeCall& a);
-int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count);
+int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count, int* rows);
 int tree_merge_comps(int d_kv, int cl, int parts);
 int tree_value_range(int parts);
 cudaError_t launch_tree_value(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st);

@@ -6,7 +6,8 @@
 // has fp32 outputs), fp32 accumulation in tensor memory.  The CL partial products meet in distributed shared memory, 128 / CL columns per CTA.
 // What bounds it is the way of the partial sums (4 d_kv bytes per row and split) into the SMs, and for few rows the chain of reads, which a
 // cluster of eight shortens; with many rows the exchange would cost more than the rest (64 KiB per CTA of eight), so CL is the largest that leaves
-// two CTAs per SM.  The decode merge does the product by FMAs, which for hundreds of nodes cost several times the reads (256 nodes of 32
+// two CTAs per SM.  Where a cluster of eight leaves room, its CTAs take 64 or 32 of their 128 rows (one tree of 16 nodes, 32 splits: 60 us with 128,
+// 58 with 64, 42 with 32; the products' idle rows cost nothing that shows).  The decode merge does the product by FMAs, which for hundreds of nodes cost several times the reads (256 nodes of 32
 // heads 373 us by a CTA per row).
 // chain_start() stands behind the allocation of tensor memory: two CTAs of this kernel share an SM, so the next kernel of the chain must
 // not find columns free that one of them still needs.
@@ -21,8 +22,9 @@ using namespace tc;
 constexpr int TM_THREADS = 256;
 constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 components] of one part
 constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // two parts of up to 128 components (three of 64); their rows of U_V^-1, 128 columns
-constexpr int TM_FEW = 4;                                     // splits whose weights are looked up once per row
-constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16 + TM_FEW * TREE_MAX_RANGES * 4 + TM_FEW) + 64;
+constexpr int TM_LEAST = 32;                                  // least rows of a CTA
+constexpr int TM_TABLE = 4 * TILE;                              // parts whose places and weights are looked up once: four per row where a CTA has 128 rows, sixteen where it has 32
+constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16) + TM_TABLE * (TREE_MAX_RANGES * 4 + 8) + 64;
 static_assert(2 * TM_SMEM <= 228 * 1024 - 2 * 1024, "two CTAs per SM");
 static_assert(TREE_MAX_SPLITS <= 64, "two splits per lane");
 static_assert(TILE * HEAD_DIM * 4 <= TM_A, "the partial products arrive where the A operand was");
@@ -33,22 +35,25 @@ template <bool BF16, int PARTS, int CL>
 __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
-  float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE, *s_w = s_inv + TILE;      // per row
-  int4* s_row = reinterpret_cast<int4*>(s_w + TILE * TM_FEW * TREE_MAX_RANGES);                     // first part, splits, request, row of the outputs; -1: none
-  unsigned char* s_cls = reinterpret_cast<unsigned char*>(s_row + TILE);
-  unsigned char* tail = s_cls + TILE * TM_FEW;
+  float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE;             // per row
+  int4* s_row = reinterpret_cast<int4*>(s_inv + TILE);                                              // first part, splits, request, row of the outputs; -1: none
+  float4* s_w = reinterpret_cast<float4*>(s_row + TILE);                                            // per row and split: what its part is worth, per range of panels;
+  int2* s_part = reinterpret_cast<int2*>(s_w + TM_TABLE);                                           // the part, its components
+  unsigned char* tail = reinterpret_cast<unsigned char*>(s_part + TM_TABLE);
   const uint32_t b_full = smem_addr(tail), done = b_full + 8;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(tail + 16);
   volatile int* abort_flag = reinterpret_cast<int*>(s_tmem + 1);
+  int* s_used = reinterpret_cast<int*>(s_tmem + 2);                                    // most splits of a row
   constexpr uint32_t PART = PARTS == 3 ? TM_PANEL : 2 * TM_PANEL;                     // bytes of one part of the A operand
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int c = CL > 1 ? (int)cluster_cta_rank() : 0, g = blockIdx.y, rep = v.rep, jn = a.m_comps;      // components at a time: a multiple of 16, at most 128
-  const int slot0 = (blockIdx.x / CL) * (TILE / rep), n_slots = a.n_req * a.T;
+  const int slots = a.m_rows / rep, slot0 = (blockIdx.x / CL) * slots, n_slots = min(slot0 + slots, a.n_req * a.T);
   const bool misaligned = (sA & 1023u) != 0;
   if (tid == 0) {
     mbar_init(b_full, 1);
     mbar_init(done, 1);
     *abort_flag = misaligned ? 1 : 0;
+    *s_used = 0;
     mbar_init_fence();
   }
   if (warp == 1) tmem_alloc(smem_addr(s_tmem), 128);
@@ -58,74 +63,83 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   chain_start();
   const uint32_t tmem = *s_tmem;
   chain_wait();
-  // A thread per row (slot, h), slot = request * T + node: where its parts are, the largest reference of its splits, one over the sum of all weights;
-  // and what the parts of the first splits are worth.  The components of a range of panels have a reference of their own; behind a split's
-  // widest class there are none.  Looked up here once, so that the reads below depend on shared memory only.
-  if (tid < TILE) {
-    const int slot = slot0 + tid / rep, req = slot / a.T, t = slot - req * a.T;
-    int row = -1, used = 0;
+  // Two to eight lanes per row (slot, h), slot = request * T + node: where its parts are, the largest reference of its splits, one over the sum of all
+  // weights; and what the parts are worth, where the table holds them.  The components of a range of panels have a reference of their own; behind a
+  // split's widest class there are none.  Looked up here once, so that the reads below depend on shared memory only.
+  const int few = TM_TABLE / a.m_rows;
+  {
+    const int lanes = TM_THREADS / a.m_rows, r = tid / lanes, j = tid % lanes;
+    const int slot = slot0 + r / rep, req = slot / a.T, t = slot - req * a.T;
+    const int4 info = slot < n_slots ? a.info[req] : make_int4(0, 0, 0, 0);
+    const bool in = slot < n_slots && t < info.y;
+    const int row = in ? slot * a.n_splits * v.Hq + g * rep + r % rep : -1, used = in ? info.w : 0;      // splits that hold something come first
     float most = -INFINITY, sum = 0.f;
-    int4 info = make_int4(0, 0, 0, 0);
-    if (slot < n_slots) info = a.info[req];
-    if (slot < n_slots && t < info.y) {
-      used = info.w;                                            // splits that hold something come first
-      row = slot * a.n_splits * v.Hq + g * rep + tid % rep;
-      const float4* refs = a.part_m + row;
-      const float* sums = a.part_l + row;
-      for (int s0 = 0; s0 < used; s0 += 4) {
-        float4 y[4];
-        float l[4];
+    for (int s0 = j; s0 < used; s0 += 4 * lanes) {
+      float4 y[4];
+      float l[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          y[k] = s0 + k < used ? refs[(size_t)(s0 + k) * v.Hq] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-          l[k] = s0 + k < used ? sums[(size_t)(s0 + k) * v.Hq] : 0.f;
-        }
-        const float m = fmaxf(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), most);
-        sum *= most == -INFINITY ? 0.f : tm_ex2(most - m);      // (one that is not a number stays one)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sum += l[k] * (y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m));
-        most = m;
-        if (used <= TM_FEW) {
-#pragma unroll
-          for (int k = 0; k < TM_FEW; ++k) {
-            s_cls[tid * TM_FEW + k] = k < used ? (unsigned char)a.part_cls[req * a.n_splits + k] : 0;
-            const float ref[TREE_MAX_RANGES] = {y[k].x, y[k].y, y[k].z, y[k].w};
-#pragma unroll
-            for (int e = 0; e < TREE_MAX_RANGES; ++e) s_w[(tid * TM_FEW + k) * TREE_MAX_RANGES + e] = ref[e] == -INFINITY ? 0.f : tm_ex2(ref[e] - m);
-          }
-        }
+      for (int k = 0; k < 4; ++k) {
+        const int sp = s0 + k * lanes;
+        y[k] = sp < used ? a.part_m[row + (size_t)sp * v.Hq] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        l[k] = sp < used ? a.part_l[row + (size_t)sp * v.Hq] : 0.f;
       }
+      const float m = fmaxf(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), most);
+      sum *= most == -INFINITY ? 0.f : tm_ex2(most - m);        // (one that is not a number stays one)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        sum += l[k] * (y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m));
+        if (s0 + k * lanes < few) s_w[r * few + s0 + k * lanes] = y[k];
+      }
+      most = m;
     }
-    s_row[tid] = make_int4(row, used, req, slot < n_slots && t < info.y ? info.x + t : -1);
-    s_most[tid] = most;
+    float all = most;
+    for (int o = lanes / 2; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
+    sum *= most == -INFINITY ? 0.f : tm_ex2(most - all);
+    for (int o = lanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     // 0: no token seen.  (With what the products' sum is expected to lose.)
-    s_inv[tid] = sum == 0.f ? 0.f : (1.f + TREE_CUT * (float)(v.d_kv / CL / 16 * PARTS)) / sum;
+    const float inv = sum == 0.f ? 0.f : (1.f + TREE_CUT * (float)(v.d_kv / CL / 16 * PARTS)) / sum;
+    for (int k = j; k < few; k += lanes) {
+      s_part[r * few + k] = k < used ? make_int2(row + k * v.Hq, a.part_cls[req * a.n_splits + k] * PANEL) : make_int2(0, 0);
+      if (k >= used) continue;
+      const float4 y = s_w[r * few + k];
+      s_w[r * few + k] = make_float4(y.x == -INFINITY ? 0.f : tm_ex2(y.x - all) * inv, y.y == -INFINITY ? 0.f : tm_ex2(y.y - all) * inv,
+                                     y.z == -INFINITY ? 0.f : tm_ex2(y.z - all) * inv, y.w == -INFINITY ? 0.f : tm_ex2(y.w - all) * inv);
+    }
+    if (j == 0) {
+      s_row[r] = make_int4(row, used, req, in ? info.x + t : -1);
+      s_most[r] = all;
+      s_inv[r] = inv;
+      if (used > 0) atomicMax(s_used, used);
+    }
   }
   __syncthreads();
-  // Sums: a warp takes rows warp, warp + 8, ..., its lanes four components.  Eight reads on their way: of as many rows where a row has few splits, of
-  // eight splits otherwise.  (16384 rows of one split one after the other took 204 us.)
-  const bool mine = lane * 4 < jn;
-  auto put = [&](int r, float4 x) {                             // a row's normalised components as the A operand
+  // Sums: a lane takes four components of a row; a warp rows warp, warp + 8, ..., two at a time where half of its lanes are enough for one.  Eight reads on
+  // their way: of as many rows where the table has the row's splits, of eight splits otherwise.  (16384 rows of one split one after the other took 204 us.)
+  // What bounds it is the issue of instructions, so places and weights come from the table, and no lane is idle (37 trees of 13 nodes, fp32 outputs: 31 us
+  // with a look-up per row and part and 16 idle lanes, 21 us so; 20 trees of 4 nodes, three splits: 32 and 24 us).
+  const int fold = jn <= 64 ? 2 : 1, e0 = (lane & (32 / fold - 1)) * 4, its = a.m_rows / 8 / fold;
+  const int r0 = warp + (fold == 2 ? (lane >> 4) * 8 : 0);         // row of iteration i: r0 + 8 fold i, so its place in a swizzled group of eight rows is warp
+  const bool mine = e0 < jn;
+  unsigned char* const dst0 = smem + (e0 >> 6) * TM_PANEL + r0 * 128 + ((((e0 >> 3) & 7) ^ warp) << 4) + (e0 & 7) * 2;
+  auto put = [&](int i, float4 x) {                             // a row's normalised components as the A operand
     if (!mine) return;
-    const float il = s_inv[r];
     uint32_t w[PARTS][2];                                       // the largest part first
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       uint64_t y;
-      asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"((h ? x.z : x.x) * il), "f"((h ? x.w : x.y) * il));
+      asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(h ? x.z : x.x), "f"(h ? x.w : x.y));
       if constexpr (PARTS == 3) tree_split3(y, w[0][h], w[1][h], w[2][h]);
       else split_pair_16<BF16>(y, w[0][h], w[1][h]);
     }
-    const int e = lane * 4;
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p)
-      *reinterpret_cast<uint2*>(smem + p * PART + (e >> 6) * TM_PANEL + r * 128 + ((((e >> 3) & 7) ^ (r & 7)) << 4) + (e & 7) * 2) = make_uint2(w[p][0], w[p][1]);
+    for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint2*>(dst0 + p * PART + i * fold * 1024) = make_uint2(w[p][0], w[p][1]);
   };
+  const int used = *s_used;
   bool ok = !misaligned;
   uint32_t ph = 0;
   const int first = c * (v.d_kv / CL), n_chunks = v.d_kv / CL / jn;
   for (int chunk = 0; chunk < n_chunks; ++chunk) {
-    const int j0 = first + chunk * jn, comp = j0 + lane * 4, range = comp / (a.range * PANEL);
+    const int j0 = first + chunk * jn, comp = j0 + e0, range = comp / (a.range * PANEL);
     if (warp == 0 && elect_one() && ok) {                      // U_V^-1, on its way while the splits are summed
       mbar_expect_tx(b_full, (uint32_t)jn * 256u);
       tma_load_2d(sB, &map_uv, b_full, g * HEAD_DIM, j0);
@@ -133,42 +147,46 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     }
     __syncwarp();
     const float* const acc = a.part_acc + comp;
-    if (a.n_splits <= TM_FEW) {
+    if (used <= few) {
+      const float* const s_wr = reinterpret_cast<const float*>(s_w) + range;
 #pragma unroll 1
-      for (int b = 0; b < TILE / 8; b += 8) {
+      for (int i0 = 0; i0 < its; i0 += 8) {
         float4 x[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        const int at = (r0 + 8 * fold * i0) * few;
 #pragma unroll 1
-        for (int s = 0; s < a.n_splits; ++s) {
+        for (int s = 0; s < used; ++s) {
           float4 y[8];
+          float w[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const int r = warp + 8 * (b + k);
-            const int4 q = s_row[r];
-            const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
-            y[k] = in ? *reinterpret_cast<const float4*>(acc + (size_t)(q.x + s * v.Hq) * v.d_kv) : make_float4(0.f, 0.f, 0.f, 0.f);
+            y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+            w[k] = 0.f;
+            if (i0 + k < its) {
+              const int n = at + 8 * fold * k * few + s;
+              const int2 part = s_part[n];
+              if (mine && comp < part.y) {
+                y[k] = *reinterpret_cast<const float4*>(acc + (size_t)part.x * v.d_kv);
+                w[k] = s_wr[4 * n];
+              }
+            }
           }
 #pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int r = warp + 8 * (b + k);
-            const int4 q = s_row[r];
-            const bool in = mine && q.x >= 0 && s < q.y && comp < s_cls[r * TM_FEW + s] * PANEL;
-            const float w = in ? s_w[(r * TM_FEW + s) * TREE_MAX_RANGES + range] : 0.f;
-            x[k].x += y[k].x * w; x[k].y += y[k].y * w; x[k].z += y[k].z * w; x[k].w += y[k].w * w;
-          }
+          for (int k = 0; k < 8; ++k) { x[k].x += y[k].x * w[k]; x[k].y += y[k].y * w[k]; x[k].z += y[k].z * w[k]; x[k].w += y[k].w * w[k]; }
         }
 #pragma unroll
-        for (int k = 0; k < 8; ++k) put(warp + 8 * (b + k), x[k]);
+        for (int k = 0; k < 8; ++k)
+          if (i0 + k < its) put(i0 + k, x[k]);
       }
     } else {
 #pragma unroll 1
-      for (int r = warp; r < TILE; r += TM_THREADS / 32) {
-        const int4 q = s_row[r];
-        if (q.x < 0) continue;
+      for (int i = 0; i < its; ++i) {
+        const int r = r0 + 8 * fold * i;
+        const int4 q = s_row[r];                                  // (no row: no splits)
         const int* cls = a.part_cls + q.z * a.n_splits;
-        const float* refs = reinterpret_cast<const float*>(a.part_m + q.x) + range;
-        const float most = s_most[r];
+        const float* refs = reinterpret_cast<const float*>(a.part_m + max(q.x, 0)) + range;
+        const float most = s_most[r], inv = s_inv[r];
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
         for (int s0 = 0; s0 < q.y; s0 += 8) {
@@ -186,7 +204,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
             x.x += y[k].x * w; x.y += y[k].y * w; x.z += y[k].z * w; x.w += y[k].w * w;
           }
         }
-        put(r, x);
+        put(i, make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
       }
     }
     fence_proxy_async_smem();
@@ -213,7 +231,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   }
   constexpr int CW = HEAD_DIM / CL;                             // columns a CTA writes
   if constexpr (CL > 1) cluster_sync_all();                     // every CTA's A operand has been used: the parts may arrive there
-  {
+  if ((warp & 3) * 32 < a.m_rows) {
     const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
     float x[32];
 #pragma unroll
@@ -243,7 +261,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   if (warp == 1) tmem_dealloc(tmem, 128);
   {
     const int r = tid & (TILE - 1), e0 = (tid >> 7) * (CW / 2);
-    const int4 q = s_row[r];
+    const int4 q = r < a.m_rows ? s_row[r] : make_int4(0, 0, 0, -1);
     if (q.w >= 0) {
       const bool bad = q.y > 0 && (a.masks[q.w] & a.bad[q.z]);    // sees a node whose value is not finite
 #pragma unroll 2
@@ -281,11 +299,13 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   if (tid == 0 && *abort_flag) set_status(v, misaligned ? TWKV_ERR_DEVICE_CHECK : TWKV_ERR_TIMEOUT);
 }
 
-// CTAs of a cluster: as many as leave two CTAs per SM.
-int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count) {
-  const int work = (a.n_req * a.T * v.rep + TILE - 1) / TILE * v.Hkv;
+// CTAs of a cluster, and rows that one takes: as many and as few as leave two CTAs per SM.
+int tree_merge_cluster(const DevView& v, const TreeCall& a, int sm_count, int* rows) {
+  auto tiles = [&](int rows) { return (a.n_req * a.T + rows / v.rep - 1) / (rows / v.rep) * v.Hkv; };
   int cl = 8;
-  while (cl > 1 && work * cl > 2 * sm_count) cl /= 2;
+  while (cl > 1 && tiles(TILE) * cl > 2 * sm_count) cl /= 2;
+  *rows = TILE;
+  while (*rows > TM_LEAST && *rows / 2 >= v.rep && tiles(*rows / 2) * cl <= 2 * sm_count) *rows /= 2;
   return cl;
 }
 // Components that a CTA takes at a time: the least number of equal pieces of at most 128 (three parts: 64), a multiple of sixteen each.
@@ -300,7 +320,7 @@ template <bool BF16, int PARTS, int CL>
 static cudaError_t launch_tree_merge_t(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(tree_merge_kernel<BF16, PARTS, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TM_SMEM);
   if (e != cudaSuccess) return e;
-  const int tiles = (a.n_req * a.T * v.rep + TILE - 1) / TILE;
+  const int slots = a.m_rows / v.rep, tiles = (a.n_req * a.T + slots - 1) / slots;
   return launch_chained(tree_merge_kernel<BF16, PARTS, CL>, dim3(CL * tiles, v.Hkv), dim3(TM_THREADS), dim3(CL), TM_SMEM, st, maps.uv, v, a);
 }
 template <bool BF16, int PARTS>

@@ -253,23 +253,45 @@ __device__ void tree_klist(const DevView& v, const TreeCall& a, int layer, int n
   }
 }
 
-// Cut points of a request's V tiles, the nodes' last, into splits of about equal cost, as for a decode pass; a split gets at least four tiles' worth.
-__device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int i, const int4& r) {
-  __shared__ int s_warp[32];
+constexpr float TREE_CTA_COST = 200.f;
+// Estimated time of the value kernel and the merge with s splits, all requests taken to be like this one; in the time of a panel's product with a
+// sixteen-token box (44 ns).  work: of a request's tiles, per range of panels.  A CTA costs as much as four tiles before and behind them, CTAs come to the SMs
+// as these get free, and the merge reads every split's sums at 3 TB/s.  Value kernel and merge in us by splits, the choice last: 16 sequences of 2048
+// tokens, 8 nodes: 1: 79, 2: 64, 4: 76, 2; 20 of 3000, 4 nodes: 1: 114, 3: 80, 7: 107, 2 or 3; one of 16384, 16 nodes: 8: 70, 16: 61, 32: 81, 16; 8 of 4096: 2: 74,
+// 4: 61, 9: 79, 3; one of 65536, 4 nodes: 16: 94, 64: 71, 32 to 64.
+__device__ __forceinline__ float tree_splits_cost(const DevView& v, const TreeCall& a, const int* work, int sms, int s) {
+  const float groups = (float)(a.n_req * ((a.C + TILE - 1) / TILE)), inv = 1.f / (float)s;
+  float all = 0.f, longest = 0.f;
+  int panels = 0;
+  for (int z = 0; z < TREE_MAX_RANGES; ++z) {
+    if (work[z] == 0) continue;
+    all += (float)work[z] + TREE_CTA_COST * (float)s;
+    longest = fmaxf(longest, (float)work[z] * inv + TREE_CTA_COST);
+    panels += a.range;
+  }
+  const float bytes = (float)(a.n_req * a.T * v.Hq) * (float)(min(panels, v.NC) * PANEL * 4);
+  return fmaxf(longest, groups * all / (float)sms + 0.3f * longest) + (float)s * (8.f + bytes * 7.5e-6f);
+}
+
+// Cut points of a request's V tiles, the nodes' last, into splits of about equal cost, as for a decode pass.
+__device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int i, const int4& r, int sms) {
+  __shared__ int s_warp[32], s_work[TREE_MAX_RANGES];
+  __shared__ unsigned long long s_best;
   const int tid = threadIdx.x, n_splits = a.n_splits;
   int* cut = a.vcut + (size_t)i * (n_splits + 1);
   const int nv = r.z >= 0 && r.y > 0 ? v.svc(layer)[r.z] : 0, n = r.z >= 0 && r.y > 0 ? nv + 1 : 0;
-  const int used = n > 0 ? min(n_splits, max(1, n / 4)) : 0;
-  if (tid == 0) a.info[i] = make_int4(r.x, r.y, r.z, used);
   if (n == 0) {
+    if (tid == 0) a.info[i] = make_int4(r.x, r.y, r.z, 0);
     for (int s = tid; s <= n_splits; s += 1024) cut[s] = 0;
     return;
   }
+  if (tid < TREE_MAX_RANGES) s_work[tid] = 0;
+  if (tid == 0) s_best = ~0ull;
   const int* list = v.svt(layer) + (size_t)r.z * v.TPS;
   const int4* desc = v.desc(layer, 1);
   const int stride = vtile_stride(nv);
   int4* meta = a.vmeta + (size_t)i * (v.TPS + 1);
-  auto cost = [&](int k) -> int {
+  auto cost = [&](int k, bool count) -> int {
     if (k >= n) return 0;
     int4 m;
     if (k < nv) {
@@ -281,19 +303,31 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
     }
     meta[k] = m;
     // in panels' products: a tile's weights take as long as those of four panels; wide tiles are taken in ranges, by CTAs of their own
-    return vtile_boxes(m.z) * max(min(m.y, a.range), 4) + 4;
+    auto of_range = [&](int z) { return m.y > z * a.range ? vtile_boxes(m.z) * max(min(m.y - z * a.range, a.range), 4) + 4 : 0; };
+    if (count)
+      for (int z = 1; z < TREE_MAX_RANGES && m.y > z * a.range; ++z) atomicAdd(&s_work[z], of_range(z));
+    return of_range(0);
   };
   int total = 0;
   for (int k0 = 0; k0 < n; k0 += 1024) {
     int part;
-    block_scan_excl(cost(k0 + tid), s_warp, &part);
+    block_scan_excl(cost(k0 + tid, true), s_warp, &part);
     total += part;
   }
+  if (tid == 0) s_work[0] = total;
+  __syncthreads();
+  if (tid < min(n_splits, n)) {
+    const float us = tree_splits_cost(v, a, s_work, sms, tid + 1);
+    atomicMin(&s_best, (unsigned long long)__float_as_uint(us) << 32 | (unsigned)(tid + 1));
+  }
+  __syncthreads();
+  const int used = (int)(s_best & 0xffffffffull);
+  if (tid == 0) a.info[i] = make_int4(r.x, r.y, r.z, used);
   const unsigned long long W = (unsigned long long)total, ns = (unsigned long long)used;
   int base = 0;
   for (int k0 = 0; k0 < n; k0 += 1024) {
     int part;
-    const int w = cost(k0 + tid);
+    const int w = cost(k0 + tid, false);
     const int off = base + block_scan_excl(w, s_warp, &part);
     base += part;
     if (k0 + tid < n) {
@@ -395,7 +429,7 @@ __device__ void tree_links(const DevView& v, const TreeCall& a, int layer, int i
   }
 }
 
-__global__ void __launch_bounds__(1024) tree_plan_kernel(DevView v, TreeCall a, int layer, int n_pieces, int vj, int qc) {
+__global__ void __launch_bounds__(1024) tree_plan_kernel(DevView v, TreeCall a, int layer, int n_pieces, int vj, int qc, int sms) {
   __shared__ int4 s_r;
   chain_start();
   chain_wait();
@@ -415,7 +449,7 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(DevView v, TreeCall a, 
   const int4 r = tree_distinct(a, i, s_r);
   if (job == 0) {
     if (r.z < 0 && threadIdx.x == 0) set_status(v, TWKV_ERR_INVALID_ARG);
-    tree_vsplit(v, a, layer, i, r);
+    tree_vsplit(v, a, layer, i, r, sms);
   } else if (job == 1) {
     if (r.z < 0 || threadIdx.x >= TWKV_MAX_CLASSES / 2 * 32) return;
     const unsigned masks = joint_masks(v, layer, r.z);
@@ -431,14 +465,14 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(DevView v, TreeCall a, 
   }
 }
 
-cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int n_pieces, cudaStream_t st) {
+cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int n_pieces, int sm_count, cudaStream_t st) {
   ProfScope ps(TWKV_K_PLAN, st);
   const int vj = a.n_req >= 128 ? 1 : std::min(64, (256 - a.n_req) / a.n_req);
   const int qc = std::max(1, std::min(8, v.Hkv * a.Rp * 16 / 4096));
   const size_t smem = tree_plan_smem(v.S, a.n_req);
   cudaError_t e = cudaFuncSetAttribute(tree_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  e = launch_chained(tree_plan_kernel, dim3(v.NC + a.n_req * (4 + vj + qc)), dim3(1024), dim3(1), smem, st, v, a, layer, n_pieces, vj, qc);
+  e = launch_chained(tree_plan_kernel, dim3(v.NC + a.n_req * (4 + vj + qc)), dim3(1024), dim3(1), smem, st, v, a, layer, n_pieces, vj, qc, sm_count);
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaGetLastError();
