@@ -95,26 +95,27 @@ __device__ __forceinline__ int tree_tiles(int fill, unsigned joint, int k, int n
 
 struct TreeSmem {          // of the class CTAs, behind one another in dynamic shared memory
   int *first;              // [S] first request of the call that names the sequence
-  int *base, *cur;         // [n_req] first entry of the request, next entry of this class
+  int *base, *cur;         // [n_req] first entry of the request (tiles of the request until it is known), next entry of this class
+  int* mine;               // [n_req] tiles in this class
   int *node;               // [n_req] class of the nodes' keys, 0: the request has no entries
   unsigned* joint;         // [n_req]
   unsigned long long* cost;    // [n_req + 1] (first class CTA) estimated cost of the requests before
 };
-static size_t tree_plan_smem(int S, int n_req) { return (size_t)S * 4 + (size_t)n_req * 16 + (size_t)(n_req + 2) * 8 + 16; }
+static size_t tree_plan_smem(int S, int n_req) { return (size_t)S * 4 + (size_t)n_req * 20 + (size_t)(n_req + 2) * 8 + 16; }
 
 __device__ void tree_klist(const DevView& v, const TreeCall& a, int layer, int n_pieces) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int s_warp[32];
-  __shared__ unsigned long long s_wide;
+  __shared__ unsigned s_wide;
   __shared__ int s_hg;
   TreeSmem s;
   s.cost = reinterpret_cast<unsigned long long*>(smem);
   s.first = reinterpret_cast<int*>(s.cost + a.n_req + 2);
-  s.base = s.first + v.S; s.cur = s.base + a.n_req; s.node = s.cur + a.n_req; s.joint = reinterpret_cast<unsigned*>(s.node + a.n_req);
+  s.base = s.first + v.S; s.cur = s.base + a.n_req; s.mine = s.cur + a.n_req; s.node = s.mine + a.n_req; s.joint = reinterpret_cast<unsigned*>(s.node + a.n_req);
   const int NC = v.NC, run = blockIdx.x, cls = NC - run, tid = threadIdx.x, warp = tid >> 5;
   const int* fill = v.fill_l(layer);
   for (int i = tid; i < v.S; i += 1024) s.first[i] = 0x7fffffff;
-  if (tid == 0) s_wide = 0ull;
+  if (tid == 0) s_wide = 0u;
   __syncthreads();
   for (int i0 = 0, most = INT_MIN; i0 < a.r0 + a.n_req; i0 += 1024) {
     const int i = i0 + tid;
@@ -127,47 +128,56 @@ __device__ void tree_klist(const DevView& v, const TreeCall& a, int layer, int n
     if (in && i >= a.r0) s.cur[i - a.r0] = before > off;            // an earlier request reaches into this one's rows
   }
   __syncthreads();
+  // a warp per request, a lane per class
   for (int i = warp; i < a.n_req; i += 32) {
     const int4 r = tree_request(v, a, i);
-    const bool ok = r.z >= 0 && r.y > 0 && s.first[r.z] == a.r0 + i && !s.cur[i];
-    if ((tid & 31) == 0) s.node[i] = ok ? r.w & 0xff : 0;
+    const int lane = tid & 31, k = lane;
+    const int node = r.z >= 0 && r.y > 0 && s.first[r.z] == a.r0 + i && !s.cur[i] ? r.w & 0xff : 0;
+    unsigned joint = 0u, cost = 0u;
+    int c = 0, before = 0;
+    if (node) {
+      joint = joint_masks(v, layer, r.z);
+      c = k < NC ? tree_tiles(fill[(size_t)r.z * NC + k], joint, k, node) : 0;
+      before = c;                                                  // tiles in this class and wider ones
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int u = __shfl_down_sync(0xffffffffu, before, o);
+        if (lane + o < 32) before += u;
+      }
+      if (run == 0) {
+        const int items = (before + 1) / 2 - (before - c + 1) / 2;  // whose wider tile has this class
+        cost = items ? tree_cost(v, a, k + 1) : 0u;
+        const unsigned wide = __reduce_max_sync(0xffffffffu, cost);
+        if (lane == 0) atomicMax(&s_wide, wide);
+        cost = __reduce_add_sync(0xffffffffu, cost * (unsigned)items);     // (2^20 tokens of eight heads are below 2^31)
+      }
+    }
+    __syncwarp();
+    if (lane == 0) {
+      s.node[i] = node;
+      s.joint[i] = joint;
+      s.base[i] = before;                                          // all of them
+      if (run == 0) s.cost[i] = cost;
+    }
+    if (lane == cls - 1) { s.cur[i] = before - c; s.mine[i] = c; }
   }
   __syncthreads();
   int base = 0;
   for (int i0 = 0; i0 < a.n_req; i0 += 1024) {
     const int i = i0 + tid;
-    const int node = i < a.n_req ? s.node[i] : 0;
-    int all = 0, wide = 0, mine = 0;
-    unsigned joint = 0u;
-    unsigned long long cost = 0ull;
-    if (node) {
-      const int seq = a.req_seqs[a.r0 + i];
-      joint = joint_masks(v, layer, seq);
-      for (int k = NC - 1; k >= 0; --k) {
-        const int c = tree_tiles(fill[(size_t)seq * NC + k], joint, k, node);
-        const int items = (all + c + 1) / 2 - (all + 1) / 2;      // items whose wider tile has this class
-        if (run == 0 && items) {
-          cost += (unsigned long long)items * tree_cost(v, a, k + 1);
-          atomicMax(&s_wide, (unsigned long long)tree_cost(v, a, k + 1));
-        }
-        if (k + 1 > cls) wide += c;
-        if (k + 1 == cls) mine = c;
-        all += c;
-      }
-    }
+    const int all = i < a.n_req ? s.base[i] : 0;
     int total;
     const int at = base + block_scan_excl((all + 1) & ~1, s_warp, &total);
     base += total;
     if (i < a.n_req) {
+      const int wide = s.cur[i];
       s.base[i] = at;
       s.cur[i] = at + wide;
-      s.joint[i] = joint;
-      if (run == 0) s.cost[i] = cost;
-    }
-    if (node == cls) {                                             // the nodes' tile, last of its class, and the filler
-      const int seq = a.req_seqs[a.r0 + i], n = a.offsets[a.r0 + i + 1] - a.offsets[a.r0 + i];
-      a.klist[at + wide + mine - 1] = make_int4(i * (v.TPS + 1) + v.svc(layer)[seq], cls | TREE_NODES | n << 16, i * NC * TREE_PANEL_ROWS, i);
-      if (all & 1) a.klist[at + all] = make_int4(0, TREE_FILLER, 0, i);
+      if (s.node[i] == cls) {                                      // the nodes' tile, last of its class, and the filler
+        const int seq = a.req_seqs[a.r0 + i], n = a.offsets[a.r0 + i + 1] - a.offsets[a.r0 + i];
+        a.klist[at + wide + s.mine[i] - 1] = make_int4(i * (v.TPS + 1) + v.svc(layer)[seq], cls | TREE_NODES | n << 16, i * NC * TREE_PANEL_ROWS, i);
+        if (all & 1) a.klist[at + all] = make_int4(0, TREE_FILLER, 0, i);
+      }
     }
   }
   __syncthreads();
