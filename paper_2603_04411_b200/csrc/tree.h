@@ -15,6 +15,10 @@ namespace twkv {
 // back as a factor 1 + TREE_CUT x instructions.  Errors of fp32 outputs, without / with it for the keys alone: 4 sequences of 700 tokens 1.3e-6 / 5.2e-7 (plain
 // fp32 sums: 6.8e-7), 2 of 8192 tokens 1.1e-6 / 6.9e-7 (1.7e-6).
 constexpr float TREE_CUT = 2.15e-8f;
+// Sums of weighted values lose a fifth less, and next to nothing to the largest of three bf16 parts, whose products have sixteen bits and mostly fit the
+// sum: two instructions of sixteen tokens count, with two parts or three.  (With 2.15e-8 and every part counted, chains of 144 and 384 instructions
+// of bf16 came out 1.4e-6 and 3.2e-6 too large, of 272 and 1024 of fp16 1.1e-6 and 4.6e-6.)
+constexpr float TREE_CUT_VALUES = 1.75e-8f;
 // Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 and 16-bit outputs: what the expectation leaves grows with the chain.
 constexpr int TREE_DRAIN_F32 = 4, TREE_DRAIN_16 = 128;
 constexpr int TREE_MAX_RANGES = 4;               // ranges of panels whose sums a CTA of the value kernel keeps

@@ -254,7 +254,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         float fc = f;
 #pragma unroll
         for (int e = 0; e < RANGE / 2; ++e)
-          if (acc == (uint32_t)e) fc = f * (1.f + TREE_CUT * (float)chain[e]);
+          if (acc == (uint32_t)e) fc = f * (1.f + TREE_CUT_VALUES * (float)chain[e]);
         float d[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (fresh) {
           tmem_ld8(lanes + c + b, reinterpret_cast<uint32_t*>(d));
@@ -357,7 +357,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         const int reach = (min(m.y, panel0 + RANGE) - panel0 + 1) >> 1;
 #pragma unroll
         for (int e = 0; e < RANGE / 2; ++e)                       // (the small parts of an accumulator's first tile come before its sum has its size)
-          if (e < reach) chain[e] += vtile_boxes(m.z) * ((touched >> e) & 1u ? PARTS : 1);
+          if (e < reach) chain[e] += vtile_boxes(m.z) * ((touched >> e) & 1u ? 2 : 1);
         touched |= (1u << reach) - 1u;
         if (any) {
 #pragma unroll
