@@ -4,13 +4,15 @@
 //   acc[c][j] = sum over the split's tokens t of p[t][c] X^_V[t][j],   p = exp(s - top[c]),   l[c] = sum of p[t][c]
 // The weights are the A operand, from tensor memory (M = 128 query rows, K = 16 tokens per instruction), and the panels of a V tile, as TMA lands
 // them, the MN-major B operand (N = 128: two panels): a panel is read from shared memory once per 128 rows and part of the weights, which
-// come as two parts of the cache type, or three where bf16 caches have fp32 outputs.  (With the panels as A and 64 columns of weights as B, both from shared memory, an instruction of half the
+// come as two parts of the cache type, or three where a bf16 cache has fp32 outputs.  (One part, with room for the weights of two tiles, gains 5 % at the most:
+// the kernel waits for memory.  With the panels as A and 64 columns of weights as B, both from shared memory, an instruction of half the
 // work took 85 cycles for its operands instead of 32: 12200 cycles per tile of sixteen panels and 64 columns.)
 // Tensor memory holds the weights of one tile (64 columns per part) and three accumulators of 128 columns: six panels (with three parts two: four).  A
 // CTA therefore takes a range of six panels (blockIdx.z); the higher ranges, which only wide tiles reach, form those tiles' weights again.
 // A tile's scores come by TMA while the tile before is worked on (read from memory by the lanes themselves, whose registers hold one tile, their
 // latency bound the kernel: 5600 cycles per narrow tile).  What a row's weights are relative to, top[c],
-// is its largest score so far, moved only when it would grow by more than 2^8 (f16 holds 2^15): the accumulators are rescaled seldom, by the
+// is its largest score so far (fp16: 2^-7 of it, so that what is 2^31 below the maximum is still more than zero), moved only when that has grown by more
+// than 2^8 (f16 holds 2^15): the accumulators are rescaled seldom, by the
 // warps that own their lanes.  The merge brings the splits' parts together.
 // Tiles that are at most half full, and the nodes' tile, are read by the boxes of sixteen rows that hold tokens.
 //
@@ -62,6 +64,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
                   const __grid_constant__ CUtensorMap map_scores, const __grid_constant__ CUtensorMap map_score_boxes, DevView v, TreeCall a) {
   constexpr int RANGE = tv_range(PARTS), COLS = RANGE * PANEL;
   constexpr uint32_t COL_P = COLS;
+  constexpr float HEAD = BF16 ? 0.f : 7.f;                       // powers of two that the largest weight has when top is set
   chain_start();
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -299,8 +302,8 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         // a wait that ran out in one warp ends the loop in the four of its quarter, here: none is left at a barrier
         if (!(ok = named_bar_and(1 + quarter, 128, ok && got))) break;
         const float most = fmaxf(fmaxf(sm[0], sm[TILE]), fmaxf(sm[2 * TILE], sm[3 * TILE])) * scale;
-        const bool grow = most > top + 8.f;                       // also the first finite maximum
-        const float next = grow ? most : top, f = next == top ? 1.f : tv_ex2(top - next);      // 0 where there was none yet
+        const bool grow = most > top + (HEAD + 8.f);              // also the first finite maximum
+        const float next = grow ? most - HEAD : top, f = next == top ? 1.f : tv_ex2(top - next);      // 0 where there was none yet
         top = next;
         const float ref = top == -INFINITY ? 0.f : top;           // (a node that sees nothing so far has no maximum: weights stay 0)
         const uint64_t nm2 = tv_pack(-ref, -ref);
