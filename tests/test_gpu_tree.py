@@ -186,6 +186,10 @@ CASES = [
     ([2000], [8], 16, 4, "f16", "bf16", 64),
     ([33] * 40, [4] * 40, 8, 4, "f16", "f32", "small"),
     ([20, 1500], [2, 31], 24, 3, "bf16", "f16", "any"),
+    ([300, 0, 140], [20, 64, 33], 32, 8, "f16", "f32", 1024),         # wide classes with many query rows
+    ([131, 40], [9, 5], 7, 7, "bf16", "f32", "any"),
+    ([131], [3], 56, 7, "f16", "f32", "any"),
+    ([700], [50], 40, 5, "bf16", "f32", "any"),
 ]
 DT = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
 
@@ -216,6 +220,47 @@ def test_one_layer_of_several_and_far_positions(B):
     want, top = b.want()
     close(out, want, top, torch.float32)
     B.twkv_cache_destroy(h)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+def test_many_tiles_behind_one_another(B, dt):
+    """More requests than there are SMs for splits: a CTA takes ten tiles, empties its accumulators on the way, and finds larger and larger scores
+    (queries eight times as large, keys growing along the positions: score error 8 x that of the derivation above)."""
+    b = Batch(15, [1250] * 90, [16, 15] * 45, hq=16, hkv=2, dt=dt, ranks=200)
+    b.q = (b.q.float() * 8).to(dt)
+    ramp = torch.linspace(0.05, 1.0, 1250).repeat(90)[:, None]
+    b.xk = (b.xk.float() * ramp).to(dt)
+    h = b.cache(B, shuffle=False)
+    out, _ = run(B, h, b)
+    assert B.twkv_cache_status(h) == B.TWKV_OK
+    want, top = b.want()
+    assert (out.double().cpu() - want).abs().max() <= 8 * REL * top
+    again, _ = run(B, h, b)
+    assert torch.equal(out, again)
+    B.twkv_cache_destroy(h)
+
+
+@pytest.mark.parametrize("dt,out_dt,nodes", [(torch.float16, torch.float32, 4), (torch.bfloat16, torch.float32, 1), (torch.bfloat16, torch.bfloat16, 24)])
+def test_many_splits(B, dt, out_dt, nodes):
+    b = Batch(16, [20000], [nodes], hq=4, hkv=2, dt=dt, out_dt=out_dt, ranks="any")
+    h = b.cache(B)
+    out, _ = run(B, h, b)
+    assert B.twkv_cache_status(h) == B.TWKV_OK
+    want, top = b.want()
+    close(out, want, top, out_dt)
+    B.twkv_cache_destroy(h)
+
+
+def test_fp32_outputs_are_as_good_as_fp32_sums(B):
+    """Relative error of the whole output.  fp32 sums of n terms, each step rounded, wander by sqrt(n) 2^-24 / sqrt(3): a key's 256 products 5.5e-7, doubled by
+    queries, scores and weights, and 1300 weighted values 1.2e-6; 4e-6 is twice their sum."""
+    for dt in (torch.float16, torch.bfloat16):
+        b = Batch(17, [1300] * 3, [12] * 3, hq=8, hkv=2, dt=dt, ranks="any")
+        h = b.cache(B)
+        out, _ = run(B, h, b)
+        want, _ = b.want()
+        assert float((out.double().cpu() - want).norm() / want.norm()) <= 4e-6
+        B.twkv_cache_destroy(h)
 
 
 def test_negative_scale_and_scores_far_apart(B):
