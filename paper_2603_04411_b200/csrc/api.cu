@@ -936,11 +936,11 @@ twkv_status twkv_tree_attn(twkv_cache* c, int layer, const void* q, const void* 
   if (((uintptr_t)q | (uintptr_t)K | (uintptr_t)V | (uintptr_t)out) % 16 || (uintptr_t)levels % 4 || (uintptr_t)masks % 8 || (uintptr_t)workspace % 256)
     return TWKV_ERR_INVALID_ARG;
   if (!c->params[layer].Uinv_k || !c->params[layer].Uinv_v) return TWKV_ERR_INVALID_ARG;
-  // as many requests to a pass as the workspace holds
+  // as many requests to a pass as the workspace holds, and as 32 bits number the score rows of
   int group = n_req;
   while (group > 0) {
     TreeCall a = tree_shape(c, group, max_nodes);
-    if (tree_layout(c, a, nullptr) <= workspace_bytes) break;
+    if (tree_layout(c, a, nullptr) <= workspace_bytes && (long long)group * (c->view.TPS + 1) * TILE <= 0x7fffffffll) break;
     group = group > 1 ? (group + 1) / 2 : 0;
   }
   if (group == 0) return TWKV_ERR_CAPACITY;

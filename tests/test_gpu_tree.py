@@ -251,6 +251,24 @@ def test_many_splits(B, dt, out_dt, nodes):
     B.twkv_cache_destroy(h)
 
 
+def test_more_requests_than_a_cta_has_threads(B):
+    n = 1500
+    b = Batch(18, [j % 5 for j in range(n)], [1 + (j % 7 == 0) for j in range(n)], hq=2, hkv=1, ranks="any", max_seqs=4096)
+    h = b.cache(B)
+    out, _ = run(B, h, b)
+    assert B.twkv_cache_status(h) == B.TWKV_OK
+    want, top = b.want()
+    close(out, want, top, torch.float32)
+    # the last names the sequence of the first
+    args = b.args()
+    args["req_seqs"][-1] = args["req_seqs"][0]
+    out, _ = run(B, h, b, args)
+    assert B.twkv_cache_status(h) == B.TWKV_ERR_INVALID_ARG
+    close(out[:b.offsets[-2]], want[:b.offsets[-2]], top, torch.float32)
+    assert (out[b.offsets[-2]:] == 0).all()
+    B.twkv_cache_destroy(h)
+
+
 def test_fp32_outputs_are_as_good_as_fp32_sums(B):
     """Relative error of the whole output.  fp32 sums of n terms, each step rounded, wander by sqrt(n) 2^-24 / sqrt(3): a key's 256 products 5.5e-7, doubled by
     queries, scores and weights, and 1300 weighted values 1.2e-6; 4e-6 is twice their sum."""
