@@ -10,16 +10,17 @@
 
 namespace twkv {
 
-// The tensor core cuts its fp32 sum toward zero after every instruction: an expected loss of half a unit in the last place, 0.36 x 2^-23 of the sum's size
-// (averaged over mantissas), and of the final sum half of that per instruction, whether the sum grows steadily or wanders.  The kernels give that expected loss
-// back as a factor 1 + TREE_CUT x instructions.  Errors of fp32 outputs, without / with it for the keys alone: 4 sequences of 700 tokens 1.3e-6 / 5.2e-7 (plain
-// fp32 sums: 6.8e-7), 2 of 8192 tokens 1.1e-6 / 6.9e-7 (1.7e-6).
+// The tensor core cuts its fp32 sum toward zero after every instruction: an expected loss of half a unit in the last place, 0.36 x 2^-23 of the sum's
+// size (averaged over mantissas), and of the final sum half of that per instruction, whether the sum grows steadily or wanders.  The kernels give that
+// expected loss back as a factor 1 + TREE_CUT x instructions.  Errors of fp32 outputs, without / with it for the keys alone: 4 sequences of 700 tokens
+// 1.3e-6 / 5.2e-7 (plain fp32 sums: 6.8e-7), 2 of 8192 tokens 1.1e-6 / 6.9e-7 (1.7e-6).
 constexpr float TREE_CUT = 2.15e-8f;
 // Sums of weighted values lose a fifth less, and next to nothing to the largest of three bf16 parts, whose products have sixteen bits and mostly fit the
 // sum: two instructions of sixteen tokens count, with two parts or three.  (With 2.15e-8 and every part counted, chains of 144 and 384 instructions
 // of bf16 came out 1.4e-6 and 3.2e-6 too large, of 272 and 1024 of fp16 1.1e-6 and 4.6e-6.)
 constexpr float TREE_CUT_VALUES = 1.75e-8f;
-// Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 and 16-bit outputs: what the expectation leaves grows with the chain.
+// Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 and 16-bit outputs: what the expectation leaves grows with the
+// chain.
 // Error and time of fp32 outputs with 4 / 8 / 16 tiles: 8 x 4096 tokens bf16 7.6e-7 170 us / 1.2e-6 153 us / 1.9e-6 140 us (plain fp32 sums 1.2e-6),
 // 16 x 2048 fp16 9.3e-7 221 us / 1.2e-6 199 us / 1.8e-6 187 us (1.2e-6).
 constexpr int TREE_DRAIN_F32 = 8, TREE_DRAIN_16 = 128;
@@ -69,8 +70,7 @@ struct TreeCall {
 };
 
 // The cache's blocks (whole panels, sixteen rows of one), the nodes' keys (128 rows) and values (sixteen rows), U_K^-1 (half panels), the
-// queries, U_V^-1 (m_comps rows, 64 columns), the
-// scores (a tile's rows or sixteen of them, v_box columns).
+// queries, U_V^-1 (m_comps rows, 64 columns), the scores (a tile's rows or sixteen of them, v_box columns).
 struct TreeMaps { CUtensorMap blocks, boxes, nodes, node_boxes, uinvT, q, uv, scores, score_boxes; };
 
 // Two fp32 (packed) as three bf16 each: the nearest value, that of the rest, that of what is left then (24 bits in all).

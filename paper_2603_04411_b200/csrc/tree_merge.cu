@@ -7,8 +7,8 @@
 // What bounds it is the way of the partial sums (4 d_kv bytes per row and split) into the SMs, and for few rows the chain of reads, which a
 // cluster of eight shortens; with many rows the exchange would cost more than the rest (64 KiB per CTA of eight), so CL is the largest that leaves
 // two CTAs per SM.  Where a cluster of eight leaves room, its CTAs take 64 or 32 of their 128 rows (one tree of 16 nodes, 32 splits: 60 us with 128,
-// 58 with 64, 42 with 32; the products' idle rows cost nothing that shows).  The decode merge does the product by FMAs, which for hundreds of nodes cost several times the reads (256 nodes of 32
-// heads 373 us by a CTA per row).
+// 58 with 64, 42 with 32; the products' idle rows cost nothing that shows).  The decode merge does the product by FMAs, which for hundreds of nodes cost
+// several times the reads (256 nodes of 32 heads 373 us by a CTA per row).
 // chain_start() stands behind the allocation of tensor memory: two CTAs of this kernel share an SM, so the next kernel of the chain must
 // not find columns free that one of them still needs.
 #include "twkv_dev.h"
@@ -23,10 +23,9 @@ constexpr int TM_THREADS = 256;
 constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 components] of one part
 constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // two parts of up to 128 components (three of 64); their rows of U_V^-1, 128 columns
 constexpr int TM_LEAST = 32;                                  // least rows of a CTA
-constexpr int TM_TABLE = 4 * TILE;                              // parts whose places and weights are looked up once: four per row where a CTA has 128 rows, sixteen where it has 32
+constexpr int TM_TABLE = 4 * TILE;                            // parts whose places and weights are looked up once: four per row of 128, sixteen of 32
 constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16) + TM_TABLE * (TREE_MAX_RANGES * 4 + 8) + 64;
 static_assert(2 * TM_SMEM <= 228 * 1024 - 2 * 1024, "two CTAs per SM");
-static_assert(TREE_MAX_SPLITS <= 64, "two splits per lane");
 static_assert(TILE * HEAD_DIM * 4 <= TM_A, "the partial products arrive where the A operand was");
 
 __device__ __forceinline__ float tm_ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
@@ -37,8 +36,9 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
   float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE;             // per row
   int4* s_row = reinterpret_cast<int4*>(s_inv + TILE);                                              // first part, splits, request, row of the outputs; -1: none
-  float4* s_w = reinterpret_cast<float4*>(s_row + TILE);                                            // per row and split: what its part is worth, per range of panels;
-  int2* s_part = reinterpret_cast<int2*>(s_w + TM_TABLE);                                           // the part, its components
+  // per row and split: what its part is worth, per range of panels; the part, its components
+  float4* s_w = reinterpret_cast<float4*>(s_row + TILE);
+  int2* s_part = reinterpret_cast<int2*>(s_w + TM_TABLE);
   unsigned char* tail = reinterpret_cast<unsigned char*>(s_part + TM_TABLE);
   const uint32_t b_full = smem_addr(tail), done = b_full + 8;
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(tail + 16);
@@ -334,7 +334,8 @@ static cudaError_t launch_tree_merge_cl(const DevView& v, const TreeCall& a, con
 }
 cudaError_t launch_tree_merge(const DevView& v, const TreeCall& a, const TreeMaps& maps, cudaStream_t st) {
   ProfScope ps(TWKV_K_MERGE, st);
-  const cudaError_t e = v.dtype != TWKV_BF16 ? launch_tree_merge_cl<false, 2>(v, a, maps, st) : a.n_parts == 3 ? launch_tree_merge_cl<true, 3>(v, a, maps, st) : launch_tree_merge_cl<true, 2>(v, a, maps, st);
+  const cudaError_t e = v.dtype != TWKV_BF16 ? launch_tree_merge_cl<false, 2>(v, a, maps, st)
+                      : a.n_parts == 3 ? launch_tree_merge_cl<true, 3>(v, a, maps, st) : launch_tree_merge_cl<true, 2>(v, a, maps, st);
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaGetLastError();

@@ -16,9 +16,11 @@
 //   warp 3      issuer of the score products (even CTA)
 //   warps 4-11  rotation and high / low split (thread = one token row x half of the RoPE frequencies)
 //   warps 12-15 scores out: masked (nodes), stored in the order of the V tiles (thread = one token row)
+// Measured: 64 sequences of 8192 tokens with 8 nodes (32 query heads, fp16) 530 us, 410 in a call by itself: the power cap, as in a decode pass.  Tensor pipe
+// 46 %, issue slots 26 % and memory 2.3 TB/s in a short call: a key's way through rebuilding, rotation, product and store bounds it there.
 // Scores are stored without their scale, which the value kernel's exponents carry (a negative scale is in the queries).
-// A class wider than eight panels runs as two passes over its panels (unless there are many query rows, see panels()), the second adding to the scores the first one stored (one addition
-// per score, in memory: its order cannot vary).
+// A class wider than eight panels runs as two passes over its panels (unless there are many query rows, see panels()), the second adding to the scores
+// the first one stored (one addition per score, in memory: its order cannot vary).
 // All waits are bounded (tc_util.cuh); a wait that runs out ends the kernel with TWKV_ERR_TIMEOUT.
 #include "twkv_dev.h"
 #include "tc_util.cuh"
@@ -158,7 +160,8 @@ tree_score_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         tma_prefetch_desc(&map_boxes);
         tma_prefetch_desc(&map_nodes);
         tma_prefetch_desc(&map_q);
-        // panels: unit w, panel j, times the unit's panels have been brought, panels so far ak (slot = ak % 8); blocks: unit lw, first panel of the pass lp, KV head lsl, block lsub
+        // panels: unit w, panel j, times the unit's panels have been brought, panels so far ak (slot = ak % 8); blocks: unit lw, first panel of the
+        // pass lp, KV head lsl, block lsub
         int w = w0, j = 0, again = 0, lw = w0, lp = 0, lsl = 0, lsub = 0;
         uint32_t ak = 0, lst = 0, lph = 0, idle = 0;
         TsUnit u = unit(w0), lu = u;

@@ -3,17 +3,18 @@
 // As in a decode pass (vacc_tc.cu) the weighted sum is taken in spectral space, for 128 query rows c = (KV head, node, head of the group):
 //   acc[c][j] = sum over the split's tokens t of p[t][c] X^_V[t][j],   p = exp(s - top[c]),   l[c] = sum of p[t][c]
 // The weights are the A operand, from tensor memory (M = 128 query rows, K = 16 tokens per instruction), and the panels of a V tile, as TMA lands
-// them, the MN-major B operand (N = 128: two panels): a panel is read from shared memory once per 128 rows and part of the weights, which
-// come as two parts of the cache type, or three where a bf16 cache has fp32 outputs.  (One part, with room for the weights of two tiles, gains 5 % at the most:
-// the kernel waits for memory.  With the panels as A and 64 columns of weights as B, both from shared memory, an instruction of half the
-// work took 85 cycles for its operands instead of 32: 12200 cycles per tile of sixteen panels and 64 columns.)
+// them, the MN-major B operand (N = 128: two panels): a panel is read from shared memory once per 128 rows and part of the weights, which come as
+// two parts of the cache type, or three where a bf16 cache has fp32 outputs.  (One part, with room for the weights of two tiles, gains 5 % at the
+// most: the weights' instructions and memory bound the kernel.  With the panels as A and 64 columns of weights as B, both from shared memory, an
+// instruction of half the work took 85 cycles for its operands instead of 32: 12200 cycles per tile of sixteen panels and 64 columns.)
 // Tensor memory holds the weights of one tile (64 columns per part) and three accumulators of 128 columns: six panels (with three parts two: four).  A
 // CTA therefore takes a range of six panels (blockIdx.z); the higher ranges, which only wide tiles reach, form those tiles' weights again.
 // A tile's scores come by TMA while the tile before is worked on (read from memory by the lanes themselves, whose registers hold one tile, their
-// latency bound the kernel: 5600 cycles per narrow tile).  What a row's weights are relative to, top[c],
-// is its largest score so far (fp16: 2^-7 of it, so that what is 2^31 below the maximum is still more than zero), moved only when that has grown by more
-// than 2^8 (f16 holds 2^15): the accumulators are rescaled seldom, by the
-// warps that own their lanes.  The merge brings the splits' parts together.
+// latency bound the kernel: 5600 cycles per narrow tile).  What a row's weights are relative to, top[c], is its largest score so far (fp16: 2^-7 of it,
+// so that what is 2^31 below the maximum is still more than zero), moved only when that has grown by more than 2^8 (f16 holds 2^15): the accumulators
+// are rescaled seldom, by the warps that own their lanes.  The merge brings the splits' parts together.
+// A tile of four panels takes 2.4 to 2.7 us (16 sequences of 32768 tokens, 128 CTAs), of which the products are 1.1: 8700 warp instructions form its
+// 16384 weights, 46 % of the issue slots of that time.
 // Tiles that are at most half full, and the nodes' tile, are read by the boxes of sixteen rows that hold tokens.
 //
 // Warp roles (640 threads, one CTA per SM): 0 TMA producer of V panels, 1 MMA issuer (owns the TMEM allocation), 2 TMA producer of scores, 4-19 weights
