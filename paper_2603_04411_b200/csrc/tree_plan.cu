@@ -115,6 +115,16 @@ __device__ void tree_klist(const DevView& v, const TreeCall& a, int layer, int n
   s.base = s.first + v.S; s.cur = s.base + a.n_req; s.mine = s.cur + a.n_req; s.node = s.mine + a.n_req; s.joint = reinterpret_cast<unsigned*>(s.node + a.n_req);
   const int NC = v.NC, run = blockIdx.x, cls = NC - run, tid = threadIdx.x, warp = tid >> 5;
   const int* fill = v.fill_l(layer);
+  // the first of this class's tiles, used at the end
+  const int n_list = v.kcc(layer)[cls - 1];
+  const int4* desc = v.desc(layer, 0);
+  const int* list = v.kct(layer) + (size_t)(cls - 1) * v.NT;
+  int tile = 0;
+  int4 d = make_int4(0, 0, 0, 0);
+  if (tid < n_list) {
+    tile = list[tid];
+    d = desc[tile];
+  }
   for (int i = tid; i < v.S; i += 1024) s.first[i] = 0x7fffffff;
   if (tid == 0) s_wide = 0u;
   __syncthreads();
@@ -123,8 +133,8 @@ __device__ void tree_klist(const DevView& v, const TreeCall& a, int layer, int n
     const bool in = i < a.r0 + a.n_req;
     const int seq = in ? a.req_seqs[i] : -1, off = in ? a.offsets[i] : INT_MIN;
     if (seq >= 0 && seq < v.S) atomicMin(&s.first[seq], i);
-    int all;
-    const int before = max(most, block_max_excl(off, s_warp, &all));
+    int all = INT_MIN, before = INT_MIN;
+    if (a.r0 + a.n_req > 1) before = max(most, block_max_excl(off, s_warp, &all));
     most = max(most, all);
     if (in && i >= a.r0) s.cur[i - a.r0] = before > off;            // an earlier request reaches into this one's rows
   }
@@ -183,16 +193,15 @@ __device__ void tree_klist(const DevView& v, const TreeCall& a, int layer, int n
   }
   __syncthreads();
   // this class's tiles
-  const int n_list = v.kcc(layer)[cls - 1];
-  const int4* desc = v.desc(layer, 0);
-  const int* list = v.kct(layer) + (size_t)(cls - 1) * v.NT;
   for (int i = tid; i < n_list; i += 1024) {
-    const int t = list[i];
-    const int4 d = desc[t];
+    if (i != tid) {
+      tile = list[i];
+      d = desc[tile];
+    }
     const int slot = s.first[d.x] - a.r0;
     if (slot < 0 || slot >= a.n_req || s.node[slot] == 0) continue;
     if (d.z < TILE && ((s.joint[slot] >> (15 + cls)) & 1u)) continue;                    // lies in a joint tile
-    a.klist[atomicAdd(&s.cur[slot], 1)] = make_int4(t, d.y | d.z << 16, d.w, slot);
+    a.klist[atomicAdd(&s.cur[slot], 1)] = make_int4(tile, d.y | d.z << 16, d.w, slot);
   }
   for (int i = tid; i < a.n_req; i += 1024) {
     const unsigned j = s.joint[i];
@@ -232,29 +241,35 @@ __device__ void tree_klist(const DevView& v, const TreeCall& a, int layer, int n
   }
   __syncthreads();
   const int hg = s_hg;
-  const unsigned long long total = s.cost[a.n_req];
+  const unsigned long long total = s.cost[a.n_req], per_piece = total / (unsigned)n_pieces;
+  const unsigned over = (unsigned)(total - per_piece * (unsigned)n_pieces);
   for (int b = tid; b < n_pieces; b += 1024) {
     int start = 0;
     if (total > 0ull) {
-      const unsigned long long key = (unsigned long long)b * total / (unsigned long long)n_pieces;
+      const unsigned long long key = (unsigned long long)b * per_piece + (unsigned)b * over / (unsigned)n_pieces;      // total b / n_pieces
       int lo = 0, hi = a.n_req - 1;                                // the last request whose cost starts at or before the key
       while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (s.cost[mid] <= key) lo = mid; else hi = mid - 1;
       }
-      unsigned long long rest = key - s.cost[lo];
-      int all = 0, item = 0;
-      unsigned long long within = 0ull;
       const int node = s.node[lo], seq = node ? a.req_seqs[a.r0 + lo] : 0;
-      for (int k = NC - 1; k >= 0 && node; --k) {
-        const int c = tree_tiles(fill[(size_t)seq * NC + k], s.joint[lo], k, node);
+      const unsigned joint = s.joint[lo];
+      int tokens[TWKV_MAX_CLASSES];                                // (read at once)
+#pragma unroll
+      for (int k = 0; k < TWKV_MAX_CLASSES; ++k) tokens[k] = k < NC && node ? fill[(size_t)seq * NC + k] : 0;
+      unsigned rest = (unsigned)(key - s.cost[lo]), within = 0u;
+      int all = 0, item = 0;
+#pragma unroll
+      for (int k = TWKV_MAX_CLASSES - 1; k >= 0; --k) {
+        if (k >= NC || !node) continue;
+        const int c = tree_tiles(tokens[k], joint, k, node);
         const int items = (all + c + 1) / 2 - (all + 1) / 2;
-        const unsigned long long one = tree_cost(v, a, k + 1);
-        if (rest < (unsigned long long)items * one) {
-          within = rest * hg / one;
+        const unsigned one = tree_cost(v, a, k + 1);
+        if (rest < (unsigned)items * one) {
+          within = rest / (one / (unsigned)hg);                    // (hg parts the KV heads, so it divides an item's cost)
           break;
         }
-        rest -= (unsigned long long)items * one;
+        rest -= (unsigned)items * one;
         item += items;
         all += c;
       }
@@ -284,10 +299,21 @@ __device__ __forceinline__ float tree_splits_cost(const DevView& v, const TreeCa
   return fmaxf(longest, groups * all / (float)sms + 0.3f * longest) + (float)s * (8.f + bytes * 7.5e-6f);
 }
 
+// vtile_stride() by a warp, a candidate per lane: of 32 numbers behind one another one is always coprime to n (there are at most 25 between two such,
+// up to 510510).  The search one after the other took 2000 to 5000 cycles.
+__device__ __forceinline__ int tree_stride(int n) {
+  if (n < 3) return 1;
+  const int first = max((int)(((long long)n * 618034ll) / 1000000ll), 1);
+  int x = first + (int)(threadIdx.x & 31), y = n;
+  while (y) { const int t = x % y; x = y; y = t; }
+  return first + __ffs(__ballot_sync(0xffffffffu, x == 1)) - 1;
+}
+
+static_assert(TREE_MAX_SPLITS == 64, "two warps");
 // Cut points of a request's V tiles, the nodes' last, into splits of about equal cost, as for a decode pass.
 __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int i, const int4& r, int sms) {
   __shared__ int s_warp[32], s_work[TREE_MAX_RANGES];
-  __shared__ unsigned long long s_best;
+  __shared__ uint2 s_best[TREE_MAX_SPLITS / 32];
   const int tid = threadIdx.x, n_splits = a.n_splits;
   int* cut = a.vcut + (size_t)i * (n_splits + 1);
   const int nv = r.z >= 0 && r.y > 0 ? v.svc(layer)[r.z] : 0, n = r.z >= 0 && r.y > 0 ? nv + 1 : 0;
@@ -297,10 +323,9 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
     return;
   }
   if (tid < TREE_MAX_RANGES) s_work[tid] = 0;
-  if (tid == 0) s_best = ~0ull;
   const int* list = v.svt(layer) + (size_t)r.z * v.TPS;
   const int4* desc = v.desc(layer, 1);
-  const int stride = vtile_stride(nv);
+  const int stride = tree_stride(nv);
   int4* meta = a.vmeta + (size_t)i * (v.TPS + 1);
   auto cost = [&](int k, bool count) -> int {
     if (k >= n) return 0;
@@ -319,31 +344,35 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
       for (int z = 1; z < TREE_MAX_RANGES && m.y > z * a.range; ++z) atomicAdd(&s_work[z], of_range(z));
     return of_range(0);
   };
-  int total = 0;
+  int total = 0, w = 0, off = 0;                                   // this thread's last tile: cost, cost of those before
   for (int k0 = 0; k0 < n; k0 += 1024) {
     int part;
-    block_scan_excl(cost(k0 + tid, true), s_warp, &part);
+    w = cost(k0 + tid, true);
+    off = total + block_scan_excl(w, s_warp, &part);
     total += part;
   }
   if (tid == 0) s_work[0] = total;
   __syncthreads();
-  if (tid < min(n_splits, n)) {
-    const float us = tree_splits_cost(v, a, s_work, sms, tid + 1);
-    atomicMin(&s_best, (unsigned long long)__float_as_uint(us) << 32 | (unsigned)(tid + 1));
+  if (tid < TREE_MAX_SPLITS) {                                      // two warps, a number of splits per thread; of equal ones the smaller
+    const unsigned est = tid < min(n_splits, n) ? __float_as_uint(tree_splits_cost(v, a, s_work, sms, tid + 1)) : 0xffffffffu;      // (positive)
+    const unsigned least = __reduce_min_sync(0xffffffffu, est), who = __ballot_sync(0xffffffffu, est == least);
+    if ((tid & 31) == 0) s_best[tid >> 5] = make_uint2(least, tid + __ffs(who));
   }
   __syncthreads();
-  const int used = (int)(s_best & 0xffffffffull);
+  const int used = (int)(s_best[1].x < s_best[0].x ? s_best[1].y : s_best[0].y);
   if (tid == 0) a.info[i] = make_int4(r.x, r.y, r.z, used);
-  const unsigned long long W = (unsigned long long)total, ns = (unsigned long long)used;
+  const unsigned W = (unsigned)total, ns = (unsigned)used;          // (4113 tiles of at most 52, 64 splits: far from 32 bits)
   int base = 0;
   for (int k0 = 0; k0 < n; k0 += 1024) {
-    int part;
-    const int w = cost(k0 + tid, false);
-    const int off = base + block_scan_excl(w, s_warp, &part);
-    base += part;
+    if (n > 1024) {
+      int part;
+      w = cost(k0 + tid, false);
+      off = base + block_scan_excl(w, s_warp, &part);
+      base += part;
+    }
     if (k0 + tid < n) {
-      const unsigned long long e = (unsigned long long)off, p = e + (unsigned long long)w;
-      for (unsigned long long s = (e * ns + W - 1ull) / W; s < ns && s * W / ns < p; ++s) cut[s] = k0 + tid;
+      const unsigned e = (unsigned)off, p = e + (unsigned)w;
+      for (unsigned s = (e * ns + W - 1u) / W; s < ns && s * W / ns < p; ++s) cut[s] = k0 + tid;
     }
   }
   for (int s = used + tid; s <= n_splits; s += 1024) cut[s] = n;
