@@ -858,6 +858,7 @@ static size_t tree_layout(const twkv_cache* c, TreeCall& a, unsigned char* base)
   a.parts = (int*)take(sizeof(int));
   a.part_m = (float4*)take(parts * sizeof(float4));
   a.part_l = (float*)take(parts * sizeof(float));
+  a.part_x = (float4*)take(parts * sizeof(float4));
   a.part_cls = (int*)take(std::max(n, fill) * sizeof(int));
   a.part_acc = (float*)take(parts * v.d_kv * sizeof(float));
   a.scores = (float*)take(n * tiles * TILE * a.C * sizeof(float));
@@ -874,7 +875,7 @@ static TreeCall tree_shape(const twkv_cache* c, int n_req, int max_nodes) {
   // Two bf16 parts carry 16 bits: 4e-6 of the outputs, which only fp32 outputs show.  Their bf16 caches take three.
   a.n_parts = v.dtype == TWKV_BF16 && v.out_dtype == TWKV_F32 ? 3 : 2;
   a.range = tree_value_range(a.n_parts);
-  a.drain = v.out_dtype == TWKV_F32 ? TREE_DRAIN_F32 : TREE_DRAIN_16;
+  a.drain = v.out_dtype != TWKV_F32 ? TREE_DRAIN_16 : v.dtype == TWKV_BF16 ? TREE_DRAIN_F32_BF16 : TREE_DRAIN_F32;
   a.n_splits = std::max(1, std::min(TREE_MAX_SPLITS, c->sm_count / (n_req * ((a.C + TILE - 1) / TILE))));
   return a;
 }

@@ -19,11 +19,11 @@ constexpr float TREE_CUT = 2.15e-8f;
 // sum: two instructions of sixteen tokens count, with two parts or three.  (With 2.15e-8 and every part counted, chains of 144 and 384 instructions
 // of bf16 came out 1.4e-6 and 3.2e-6 too large, of 272 and 1024 of fp16 1.1e-6 and 4.6e-6.)
 constexpr float TREE_CUT_VALUES = 1.75e-8f;
-// Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 and 16-bit outputs: what the expectation leaves grows with the
-// chain.
-// Error and time of fp32 outputs with 4 / 8 / 16 tiles: 8 x 4096 tokens bf16 7.6e-7 170 us / 1.2e-6 153 us / 1.9e-6 140 us (plain fp32 sums 1.2e-6),
-// 16 x 2048 fp16 9.3e-7 221 us / 1.2e-6 199 us / 1.8e-6 187 us (1.2e-6).
-constexpr int TREE_DRAIN_F32 = 8, TREE_DRAIN_16 = 128;
+// Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 outputs (of bf16 caches, whose three parts lengthen the chains) and
+// 16-bit ones: what the expectation leaves grows with the chain.  Error and time of fp32 outputs with 4 / 8 / 16 tiles: 8 x 4096 tokens bf16 7.6e-7 170 us /
+// 1.2e-6 153 us / 1.9e-6 140 us (plain fp32 sums 1.2e-6), 3 x 30745 bf16 8.1e-7 167 us / 1.4e-6 157 us (5.7e-7), 16 x 2048 fp16 9.3e-7 221 us /
+// 1.2e-6 199 us / 1.8e-6 187 us (1.2e-6).
+constexpr int TREE_DRAIN_F32 = 8, TREE_DRAIN_F32_BF16 = 4, TREE_DRAIN_16 = 128;
 constexpr int TREE_MAX_RANGES = 4;               // ranges of panels whose sums a CTA of the value kernel keeps
 constexpr int TREE_MAX_SPLITS = 64;              // of a request's V tiles
 constexpr int TREE_PANEL_ROWS = 64;              // rows of a panel of the nodes' tiles
@@ -66,6 +66,7 @@ struct TreeCall {
   float* part_acc;      // [n_req][T][n_splits][Hq][d_kv]
   float4* part_m;       // [n_req][T][n_splits][Hq] what the split's weights are relative to (powers of two), per range of panels
   float* part_l;        // [n_req][T][n_splits][Hq] sum of the split's weights
+  float4* part_x;       // [n_req][T][n_splits][Hq] size of the largest component of the split's sums, per range of panels (fp16 caches)
   int* part_cls;        // [n_req][n_splits] widest class of the split's tiles, 0: none
 };
 

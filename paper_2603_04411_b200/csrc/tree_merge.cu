@@ -24,7 +24,7 @@ constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 c
 constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // two parts of up to 128 components (three of 64); their rows of U_V^-1, 128 columns
 constexpr int TM_LEAST = 32;                                  // least rows of a CTA
 constexpr int TM_TABLE = 4 * TILE;                            // parts whose places and weights are looked up once: four per row of 128, sixteen of 32
-constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (2 * 4 + 16) + TM_TABLE * (TREE_MAX_RANGES * 4 + 8) + 64;
+constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (3 * 4 + 16) + TM_TABLE * (TREE_MAX_RANGES * 4 + 8) + 64;
 static_assert(2 * TM_SMEM <= 228 * 1024 - 2 * 1024, "two CTAs per SM");
 static_assert(TILE * HEAD_DIM * 4 <= TM_A, "the partial products arrive where the A operand was");
 
@@ -34,8 +34,8 @@ template <bool BF16, int PARTS, int CL>
 __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
-  float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE;             // per row
-  int4* s_row = reinterpret_cast<int4*>(s_inv + TILE);                                              // first part, splits, request, row of the outputs; -1: none
+  float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE, *s_back = s_inv + TILE;      // per row
+  int4* s_row = reinterpret_cast<int4*>(s_back + TILE);                                              // first part, splits, request, row of the outputs; -1: none
   // per row and split: what its part is worth, per range of panels; the part, its components
   float4* s_w = reinterpret_cast<float4*>(s_row + TILE);
   int2* s_part = reinterpret_cast<int2*>(s_w + TM_TABLE);
@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     *s_used = 0;
     mbar_init_fence();
   }
-  if (warp == 1) tmem_alloc(smem_addr(s_tmem), 128);
+  if (warp == 1) tmem_alloc(smem_addr(s_tmem), 256);
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
@@ -67,27 +67,40 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   // weights; and what the parts are worth, where the table holds them.  The components of a range of panels have a reference of their own; behind a
   // split's widest class there are none.  Looked up here once, so that the reads below depend on shared memory only.
   const int few = TM_TABLE / a.m_rows;
+  const bool two = v.out_dtype == TWKV_F32 && v.d_kv / CL > jn;    // two sums of every other chunk: long chains lose bits that fp32 outputs have
   {
     const int lanes = TM_THREADS / a.m_rows, r = tid / lanes, j = tid % lanes;
     const int slot = slot0 + r / rep, req = slot / a.T, t = slot - req * a.T;
     const int4 info = slot < n_slots ? a.info[req] : make_int4(0, 0, 0, 0);
     const bool in = slot < n_slots && t < info.y;
     const int row = in ? slot * a.n_splits * v.Hq + g * rep + r % rep : -1, used = in ? info.w : 0;      // splits that hold something come first
-    float most = -INFINITY, sum = 0.f;
+    float most = -INFINITY, sum = 0.f, size = 0.f;              // size: bound on the components, relative to most
     for (int s0 = j; s0 < used; s0 += 4 * lanes) {
       float4 y[4];
       float l[4];
+      float4 x[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int sp = s0 + k * lanes;
+        if constexpr (!BF16) x[k] = sp < used ? a.part_x[row + (size_t)sp * v.Hq] : make_float4(0.f, 0.f, 0.f, 0.f);
         y[k] = sp < used ? a.part_m[row + (size_t)sp * v.Hq] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
         l[k] = sp < used ? a.part_l[row + (size_t)sp * v.Hq] : 0.f;
       }
       const float m = fmaxf(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), most);
       sum *= most == -INFINITY ? 0.f : tm_ex2(most - m);        // (one that is not a number stays one)
+      size *= most == -INFINITY ? 0.f : tm_ex2(most - m);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        sum += l[k] * (y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m));
+        const float w = y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m);
+        sum += l[k] * w;
+        if constexpr (!BF16) {                                   // a range's components are relative to its own reference
+          const float ref[TREE_MAX_RANGES] = {y[k].x, y[k].y, y[k].z, y[k].w}, big[TREE_MAX_RANGES] = {x[k].x, x[k].y, x[k].z, x[k].w};
+          float of_split = 0.f;
+#pragma unroll
+          for (int e = 0; e < TREE_MAX_RANGES; ++e)
+            if (e * a.range < v.NC && ref[e] != -INFINITY) of_split = fmaxf(of_split, big[e] * tm_ex2(ref[e] - m));
+          size += of_split;
+        }
         if (s0 + k * lanes < few) s_w[r * few + s0 + k * lanes] = y[k];
       }
       most = m;
@@ -95,9 +108,17 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     float all = most;
     for (int o = lanes / 2; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
     sum *= most == -INFINITY ? 0.f : tm_ex2(most - all);
-    for (int o = lanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    size *= most == -INFINITY ? 0.f : tm_ex2(most - all);
+    for (int o = lanes / 2; o > 0; o >>= 1) { sum += __shfl_xor_sync(0xffffffffu, sum, o); size += __shfl_xor_sync(0xffffffffu, size, o); }
     // 0: no token seen.  (With what the products' sum is expected to lose.)
-    const float inv = sum == 0.f ? 0.f : (1.f + TREE_CUT * (float)(v.d_kv / CL / 16 * PARTS)) / sum;
+    float inv = sum == 0.f ? 0.f : (1.f + TREE_CUT * (float)(v.d_kv / CL / 16 * PARTS / (two ? 2 : 1))) / sum, back = 1.f;
+    if constexpr (!BF16) {
+      // f16 operands: the components go up to 2^14 by a power of two, which the outputs are divided by, so that the low part of small ones keeps its bits
+      const int e = (int)(__float_as_uint(size * inv) >> 23) - 127;                    // size * inv in [2^e, 2^(e + 1))
+      const int up = e > -60 && e < 60 ? 13 - e : 0;
+      back = __uint_as_float((unsigned)(127 - up) << 23);
+      inv *= __uint_as_float((unsigned)(127 + up) << 23);
+    }
     for (int k = j; k < few; k += lanes) {
       s_part[r * few + k] = k < used ? make_int2(row + k * v.Hq, a.part_cls[req * a.n_splits + k] * PANEL) : make_int2(0, 0);
       if (k >= used) continue;
@@ -109,6 +130,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
       s_row[r] = make_int4(row, used, req, in ? info.x + t : -1);
       s_most[r] = all;
       s_inv[r] = inv;
+      s_back[r] = back;
       if (used > 0) atomicMax(s_used, used);
     }
   }
@@ -213,12 +235,13 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
       if (mbar_wait(b_full, ph, abort_flag)) {
         fence_after_sync();
         constexpr uint32_t idesc = idesc_f16(BF16 ? 1 : 0, 128, 128) | (1u << 16);       // B MN-major
+        const uint32_t d = tmem + (two ? (uint32_t)(chunk & 1) * 128u : 0u);
         const uint32_t b_lo = ((sB >> 4) & 0x3fffu) | ((uint32_t)(jn * 128) >> 4 << 16);
         for (int part = PARTS - 1; part >= 0; --part)                     // the low parts first: the sum is cut after every instruction
           for (int ks = 0; ks < jn / 16; ++ks) {
             const uint32_t a_lo = kmajor_sw128_desc_lo(sA + part * PART + (ks >> 2) * TM_PANEL) + 2 * (ks & 3);
-            mma_f16_ss(tmem, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | a_lo, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u), idesc,
-                       chunk > 0 || part < PARTS - 1 || ks > 0 ? 1u : 0u);
+            mma_f16_ss(d, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | a_lo, ((uint64_t)KMAJOR_SW128_DESC_HI << 32) | (b_lo + ks * 128u), idesc,
+                       chunk > (two ? 1 : 0) || part < PARTS - 1 || ks > 0 ? 1u : 0u);
           }
         mma_commit(done);
       }
@@ -240,6 +263,13 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
       if (ok) {
         tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + col, x);
         tmem_ld_wait();
+        if (two) {
+          float y[32];
+          tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + 128 + col, y);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] += y[e];
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 32; ++e) x[e] = 0.f;
@@ -258,7 +288,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   if constexpr (CL > 1) cluster_sync_all();                     // every part has arrived; nothing remote is touched from here on
   else __syncthreads();
   fence_after_sync();
-  if (warp == 1) tmem_dealloc(tmem, 128);
+  if (warp == 1) tmem_dealloc(tmem, 256);
   {
     const int r = tid & (TILE - 1), e0 = (tid >> 7) * (CW / 2);
     const int4 q = r < a.m_rows ? s_row[r] : make_int4(0, 0, 0, -1);
@@ -274,6 +304,11 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
           const float4* in = reinterpret_cast<const float4*>(smem) + (k * CW + e1) / 4 * TILE + r;
           const float4 x = in[0], y = in[TILE];
           o[0] += x.x; o[1] += x.y; o[2] += x.z; o[3] += x.w; o[4] += y.x; o[5] += y.y; o[6] += y.z; o[7] += y.w;
+        }
+        if constexpr (!BF16) {
+          const float back = s_back[r];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] *= back;
         }
         if (bad) {
 #pragma unroll

@@ -243,7 +243,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     const int col0 = part * (COLS / 4);
     uint32_t stored = 0;
     int since = 0, chain[RANGE / 2] = {};                         // tiles, and instructions, in the accumulators
-    float kept = 1.f;
+    float kept = 1.f, largest = 0.f;                              // of the partial result, as it is stored
     auto read_out = [&](int c, float (&o)[32]) {                 // 32 of this thread's columns of the partial result
 #pragma unroll
       for (int b = 0; b < 32; b += 8)
@@ -266,6 +266,10 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) d[e] = held ? o[b + e] * kept + d[e] * fc : d[e] * fc;
+        if constexpr (!BF16) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) largest = fmaxf(largest, fabsf(d[e]));
+        }
         if (r >= 0) tv_st8(out + c + b, d);
       }
     };
@@ -384,6 +388,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     named_bar_sync(1 + quarter, 128);
     // This part's columns, a row per thread; columns that no tile reached are left alone, as is everything where no tile reached the range: the
     // merge knows it from the split's widest class.
+    largest = 0.f;
     if (ok && k > 0) {
 #pragma unroll 1
       for (int c = col0; c < col0 + COLS / 4; c += 32) {
@@ -392,7 +397,15 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         empty_onto(c, o, 1.f);
       }
     }
+    if constexpr (!BF16) {
+      s_max[(4 + part) * TILE + row] = largest;
+      named_bar_sync(1 + quarter, 128);
+    }
     if (part == 0 && r >= 0) {
+      if constexpr (!BF16) {
+        const float* const b = s_max + 4 * TILE + row;
+        reinterpret_cast<float*>(a.part_x + r)[range] = fmaxf(fmaxf(b[0], b[TILE]), fmaxf(b[2 * TILE], b[3 * TILE]));
+      }
       reinterpret_cast<float*>(a.part_m + r)[range] = top;
       if (range == 0) a.part_l[r] = (s_max[row] + s_max[TILE + row]) + (s_max[2 * TILE + row] + s_max[3 * TILE + row]);
     }
