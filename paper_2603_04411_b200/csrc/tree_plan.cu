@@ -9,7 +9,7 @@
 // tiles at once and multiplies them with the same queries, so both belong to one request; the narrower one's missing panels are zeros.
 // A request with an odd number of tiles ends with a filler.  Where a class's entries of a request start follows from the keys' token
 // counts, as in a decode pass; the order of tiles of one class inside a request depends on timing, and no result does.
-// What bounds it is the depth of its dependent reads and scans: 9 us and the launch for one request, 30 for 64 (one CTA of 1024 threads per SM, 500 CTAs).
+// What bounds it is the depth of its dependent reads and scans: 8 us and the launch for one request, 29 for 64 (one CTA of 1024 threads per SM, 500 CTAs).
 #include <algorithm>
 #include <climits>
 

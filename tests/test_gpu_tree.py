@@ -281,6 +281,23 @@ def test_fp32_outputs_are_as_good_as_fp32_sums(B):
         B.twkv_cache_destroy(h)
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -7, 2.0 ** 9])
+def test_small_and_large_values(B, scale):
+    """Powers of two in the values change nothing in the relative error (the bound is the one above): mean components far below the fp16 range's normal numbers
+    and near its end alike."""
+    for dt in (torch.float16, torch.bfloat16):
+        b = Batch(19, [1300, 60], [12, 7], hq=8, hkv=2, dt=dt, ranks="any")
+        b.xv, b.nv = (b.xv.float() * scale).to(dt), (b.nv.float() * scale).to(dt)
+        h = b.cache(B)
+        out, _ = run(B, h, b)
+        assert B.twkv_cache_status(h) == B.TWKV_OK
+        want, _ = b.want()
+        for i in range(2):
+            rows = slice(b.offsets[i], b.offsets[i + 1])
+            assert float((out[rows].double().cpu() - want[rows]).norm() / want[rows].norm()) <= 4e-6
+        B.twkv_cache_destroy(h)
+
+
 def test_negative_scale_and_scores_far_apart(B):
     # queries fifty times as large: the softmax is decided by one token (score error 50 x that of the derivation above)
     b = Batch(5, [300, 64], [9, 30])
