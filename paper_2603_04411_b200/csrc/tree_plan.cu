@@ -1,8 +1,7 @@
 // One launch prepares a pass of tree attention; its CTAs are, in this order:
 //   NC       one per rank class: the class's entries of the K list
 //   n_req    the splits of a request's V tiles
-//   n_req    the tables of its joint tiles
-//   n_req vj K slot -> score row of its cached tokens
+//   n_req vj K slot -> score row of its cached tokens; the first also the tables of its joint tiles
 //   n_req 2  the nodes' states cut to their ranks, as a tile of keys and a tile of values
 //   n_req qc its queries as the operand of the score products
 // The K list holds a request's tiles together, from the widest class to the narrowest, in items of two: a pair of CTAs rebuilds two
@@ -477,7 +476,7 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(DevView v, TreeCall a, 
   if (b < v.NC) { tree_klist(v, a, layer, n_pieces); return; }
   b -= v.NC;
   // the request of a CTA: one job after the other, each for all requests
-  const int n = a.n_req, per[5] = {1, 1, vj, 2, qc};
+  const int n = a.n_req, per[4] = {1, vj, 2, qc};
   int job = 0;
   while (b >= n * per[job]) b -= n * per[job++];
   const int i = b / per[job], part = b % per[job];
@@ -491,14 +490,14 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(DevView v, TreeCall a, 
     if (r.z < 0 && threadIdx.x == 0) set_status(v, TWKV_ERR_INVALID_ARG);
     tree_vsplit(v, a, layer, i, r, sms);
   } else if (job == 1) {
-    if (r.z < 0 || threadIdx.x >= TWKV_MAX_CLASSES / 2 * 32) return;
+    if (r.z < 0) return;
+    tree_links(v, a, layer, i, r, part, vj);
+    if (part > 0 || threadIdx.x >= TWKV_MAX_CLASSES / 2 * 32) return;
     const unsigned masks = joint_masks(v, layer, r.z);
     unsigned starts = masks & 0xffffu;
     for (int w = threadIdx.x >> 5; w > 0 && starts; --w) starts ^= 1u << (31 - __clz(starts));
     if (starts) joint_tile(v, layer, r.z, masks, 31 - __clz(starts), i * (v.NC / 2) + (threadIdx.x >> 5));
   } else if (job == 2) {
-    if (r.z >= 0) tree_links(v, a, layer, i, r, part, vj);
-  } else if (job == 3) {
     if (v.dtype == TWKV_BF16) tree_pack<true>(v, a, i, r, part); else tree_pack<false>(v, a, i, r, part);
   } else {
     if (v.dtype == TWKV_BF16) tree_queries<true>(v, a, i, r, part, qc); else tree_queries<false>(v, a, i, r, part, qc);
@@ -507,12 +506,12 @@ __global__ void __launch_bounds__(1024) tree_plan_kernel(DevView v, TreeCall a, 
 
 cudaError_t launch_tree_plan(const DevView& v, const TreeCall& a, int layer, int n_pieces, int sm_count, cudaStream_t st) {
   ProfScope ps(TWKV_K_PLAN, st);
-  const int vj = a.n_req >= 128 ? 1 : std::min(64, (256 - a.n_req) / a.n_req);
+  const int vj = a.n_req >= 128 ? 1 : std::min(std::min(64, (v.TPS + 7) / 8), (256 - a.n_req) / a.n_req);      // (a CTA takes eight tiles at a time)
   const int qc = std::max(1, std::min(8, v.Hkv * a.Rp * 16 / 4096));
   const size_t smem = tree_plan_smem(v.S, a.n_req);
   cudaError_t e = cudaFuncSetAttribute(tree_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  e = launch_chained(tree_plan_kernel, dim3(v.NC + a.n_req * (4 + vj + qc)), dim3(1024), dim3(1), smem, st, v, a, layer, n_pieces, vj, qc, sm_count);
+  e = launch_chained(tree_plan_kernel, dim3(v.NC + a.n_req * (3 + vj + qc)), dim3(1024), dim3(1), smem, st, v, a, layer, n_pieces, vj, qc, sm_count);
   if (e != cudaSuccess) return e;
   count_launch();
   return cudaGetLastError();
