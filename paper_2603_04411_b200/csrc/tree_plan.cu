@@ -322,6 +322,7 @@ __device__ void tree_vsplit(const DevView& v, const TreeCall& a, int layer, int 
     return;
   }
   if (tid < TREE_MAX_RANGES) s_work[tid] = 0;
+  __syncthreads();                                                 // before any warp adds to it
   const int* list = v.svt(layer) + (size_t)r.z * v.TPS;
   const int4* desc = v.desc(layer, 1);
   const int stride = tree_stride(nv);
