@@ -12,7 +12,8 @@ namespace twkv {
 
 // The tensor core cuts its fp32 sum toward zero after every instruction: an expected loss of half a unit in the last place, 0.36 x 2^-23 of the sum's
 // size (averaged over mantissas), and of the final sum half of that per instruction, whether the sum grows steadily or wanders.  The kernels give that
-// expected loss back as a factor 1 + TREE_CUT x instructions.  Errors of fp32 outputs, without / with it for the keys alone: 4 sequences of 700 tokens
+// expected loss back as a factor 1 + TREE_CUT x instructions, of which only those count that can have cut something: a
+// key's by its class, those of the last product by the widest class of the row's splits and by the parts that its components have.  Errors of fp32 outputs, without / with it for the keys alone: 4 sequences of 700 tokens
 // 1.3e-6 / 5.2e-7 (plain fp32 sums: 6.8e-7), 2 of 8192 tokens 1.1e-6 / 6.9e-7 (1.7e-6).
 constexpr float TREE_CUT = 2.15e-8f;
 // Sums of weighted values lose a fifth less, and next to nothing to the largest of three bf16 parts, whose products have sixteen bits and mostly fit the

@@ -24,7 +24,7 @@ constexpr uint32_t TM_PANEL = 16384;                          // [128 rows][64 c
 constexpr uint32_t TM_A = 4 * TM_PANEL, TM_B = 32768;         // two parts of up to 128 components (three of 64); their rows of U_V^-1, 128 columns
 constexpr int TM_LEAST = 32;                                  // least rows of a CTA
 constexpr int TM_TABLE = 4 * TILE;                            // parts whose places and weights are looked up once: four per row of 128, sixteen of 32
-constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (3 * 4 + 16) + TM_TABLE * (TREE_MAX_RANGES * 4 + 8) + 64;
+constexpr uint32_t TM_SMEM = TM_A + TM_B + TILE * (4 * 4 + 16) + TM_TABLE * (TREE_MAX_RANGES * 4 + 8) + 64;
 static_assert(2 * TM_SMEM <= 228 * 1024 - 2 * 1024, "two CTAs per SM");
 static_assert(TILE * HEAD_DIM * 4 <= TM_A, "the partial products arrive where the A operand was");
 
@@ -34,8 +34,8 @@ template <bool BF16, int PARTS, int CL>
 __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_constant__ CUtensorMap map_uv, DevView v, TreeCall a) {
   extern __shared__ __align__(1024) unsigned char smem[];
   const uint32_t sA = smem_addr(smem), sB = sA + TM_A;
-  float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE, *s_back = s_inv + TILE;      // per row
-  int4* s_row = reinterpret_cast<int4*>(s_back + TILE);                                              // first part, splits, request, row of the outputs; -1: none
+  float *s_most = reinterpret_cast<float*>(smem + TM_A + TM_B), *s_inv = s_most + TILE, *s_back = s_inv + TILE, *s_give = s_back + TILE;      // per row
+  int4* s_row = reinterpret_cast<int4*>(s_give + TILE);                                              // first part, splits, request, row of the outputs; -1: none
   // per row and split: what its part is worth, per range of panels; the part, its components
   float4* s_w = reinterpret_cast<float4*>(s_row + TILE);
   int2* s_part = reinterpret_cast<int2*>(s_w + TM_TABLE);
@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   // weights; and what the parts are worth, where the table holds them.  The components of a range of panels have a reference of their own; behind a
   // split's widest class there are none.  Looked up here once, so that the reads below depend on shared memory only.
   const int few = TM_TABLE / a.m_rows;
-  const bool two = v.out_dtype == TWKV_F32 && v.d_kv / CL > jn;    // two sums of every other chunk: long chains lose bits that fp32 outputs have
+  const bool exacting = v.out_dtype == TWKV_F32, two = exacting && v.d_kv / CL > jn;    // two sums of every other chunk: long chains lose bits that fp32 outputs have
   {
     const int lanes = TM_THREADS / a.m_rows, r = tid / lanes, j = tid % lanes;
     const int slot = slot0 + r / rep, req = slot / a.T, t = slot - req * a.T;
@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     const bool in = slot < n_slots && t < info.y;
     const int row = in ? slot * a.n_splits * v.Hq + g * rep + r % rep : -1, used = in ? info.w : 0;      // splits that hold something come first
     float most = -INFINITY, sum = 0.f, size = 0.f;              // size: bound on the components, relative to most
+    int wide = 0;                                               // widest class of the splits
     for (int s0 = j; s0 < used; s0 += 4 * lanes) {
       float4 y[4];
       float l[4];
@@ -85,6 +86,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
         if constexpr (!BF16) x[k] = sp < used ? a.part_x[row + (size_t)sp * v.Hq] : make_float4(0.f, 0.f, 0.f, 0.f);
         y[k] = sp < used ? a.part_m[row + (size_t)sp * v.Hq] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
         l[k] = sp < used ? a.part_l[row + (size_t)sp * v.Hq] : 0.f;
+        if (exacting && sp < used) wide = max(wide, a.part_cls[req * a.n_splits + sp]);
       }
       const float m = fmaxf(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), most);
       sum *= most == -INFINITY ? 0.f : tm_ex2(most - m);        // (one that is not a number stays one)
@@ -109,9 +111,9 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     for (int o = lanes / 2; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(0xffffffffu, all, o));
     sum *= most == -INFINITY ? 0.f : tm_ex2(most - all);
     size *= most == -INFINITY ? 0.f : tm_ex2(most - all);
+    for (int o = lanes / 2; o > 0; o >>= 1) wide = max(wide, __shfl_xor_sync(0xffffffffu, wide, o));
     for (int o = lanes / 2; o > 0; o >>= 1) { sum += __shfl_xor_sync(0xffffffffu, sum, o); size += __shfl_xor_sync(0xffffffffu, size, o); }
-    // 0: no token seen.  (With what the products' sum is expected to lose.)
-    float inv = sum == 0.f ? 0.f : (1.f + TREE_CUT * (float)(v.d_kv / CL / 16 * PARTS / (two ? 2 : 1))) / sum, back = 1.f;
+    float inv = sum == 0.f ? 0.f : 1.f / sum, back = 1.f;       // 0: no token seen
     if constexpr (!BF16) {
       // f16 operands: the components go up to 2^14 by a power of two, which the outputs are divided by, so that the low part of small ones keeps its bits
       const int e = (int)(__float_as_uint(size * inv) >> 23) - 127;                    // size * inv in [2^e, 2^(e + 1))
@@ -131,6 +133,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
       s_most[r] = all;
       s_inv[r] = inv;
       s_back[r] = back;
+      s_give[r] = (float)wide;
       if (used > 0) atomicMax(s_used, used);
     }
   }
@@ -143,6 +146,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
   const int r0 = warp + (fold == 2 ? (lane >> 4) * 8 : 0);         // row of iteration i: r0 + 8 fold i, so its place in a swizzled group of eight rows is warp
   const bool mine = e0 < jn;
   unsigned char* const dst0 = smem + (e0 >> 6) * TM_PANEL + r0 * 128 + ((((e0 >> 3) & 7) ^ warp) << 4) + (e0 & 7) * 2;
+  uint32_t seconds = 0u;                                       // rows (by iteration) that have a second part somewhere
   auto put = [&](int i, float4 x) {                             // a row's normalised components as the A operand
     if (!mine) return;
     uint32_t w[PARTS][2];                                       // the largest part first
@@ -155,6 +159,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     }
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) *reinterpret_cast<uint2*>(dst0 + p * PART + i * fold * 1024) = make_uint2(w[p][0], w[p][1]);
+    if (exacting && (w[1][0] | w[1][1]) != 0u) seconds |= 1u << i;
   };
   const int used = *s_used;
   bool ok = !misaligned;
@@ -252,10 +257,24 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
     fence_after_sync();
     __syncthreads();
   }
+  if (exacting) {
+    // fp32 outputs get back what the sums of the products are expected to lose (16-bit ones would not show it), by the instructions that had components
+    // (none behind the row's widest class): each of the first part, and of the others where the row has any (means of one token have none); those of
+    // bf16's two others count once the sum has its size, f16's, whose products are longer, at once.  Every lane of a row has seen its own components.
+    for (int o = 16 / fold; o > 0; o >>= 1) seconds |= __shfl_xor_sync(0xffffffffu, seconds, o);
+    const int i = lane & (32 / fold - 1);
+    if (i < its) {
+      const int r = r0 + 8 * fold * i, n = min(max((int)s_give[r] * PANEL - first, 0), v.d_kv / CL) / 16;
+      const int rest = PARTS == 3 ? 2 * max(n - (two ? 2 : 1) * jn / 16, 0) : n;
+      s_give[r] = 1.f + TREE_CUT * (two ? 0.5f : 1.f) * (float)(n + ((seconds >> i) & 1u ? rest : 0));
+    }
+    __syncthreads();
+  }
   constexpr int CW = HEAD_DIM / CL;                             // columns a CTA writes
   if constexpr (CL > 1) cluster_sync_all();                     // every CTA's A operand has been used: the parts may arrive there
   if ((warp & 3) * 32 < a.m_rows) {
     const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+    const float give = s_give[row];
     float x[32];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -269,6 +288,10 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
           tmem_ld_wait();
 #pragma unroll
           for (int e = 0; e < 32; ++e) x[e] += y[e];
+        }
+        if (exacting) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] *= give;
         }
       } else {
 #pragma unroll
