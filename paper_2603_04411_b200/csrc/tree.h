@@ -19,6 +19,8 @@ constexpr float TREE_CUT = 2.15e-8f;
 // Sums of weighted values lose a fifth less, and next to nothing to the largest of three bf16 parts, whose products have sixteen bits and mostly fit the
 // sum: two instructions of sixteen tokens count, with two parts or three.  (With 2.15e-8 and every part counted, chains of 144 and 384 instructions
 // of bf16 came out 1.4e-6 and 3.2e-6 too large, of 272 and 1024 of fp16 1.1e-6 and 4.6e-6.)
+// Which of them count follows from the weights (tree_value.cu).  What it cannot see are values whose sums are exact (components that few tokens have): those
+// come out too large by what is given back, 1.75e-8 for an instruction, up to the drain below.
 constexpr float TREE_CUT_VALUES = 1.75e-8f;
 // Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 outputs (of bf16 caches, whose three parts lengthen the chains) and
 // 16-bit ones: what the expectation leaves grows with the chain.  Error and time of fp32 outputs with 4 / 8 / 16 tiles: 8 x 4096 tokens bf16 7.6e-7 170 us /

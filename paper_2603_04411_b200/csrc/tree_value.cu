@@ -33,10 +33,12 @@ constexpr int TV_META = 256;                                   // tiles whose de
 constexpr int TV_STAGES = 4;
 constexpr uint32_t TV_PANEL = 16384, TV_STAGE = 2 * TV_PANEL;
 constexpr uint32_t TV_SCORES = TILE * TILE * 4;                 // a tile's scores with 128 query rows
-constexpr uint32_t TV_SMEM = TV_STAGES * TV_STAGE + TV_SCORES + TV_META * 16 + 2 * 4 * TILE * 4 + 256;
+constexpr uint32_t TV_SMEM = TV_STAGES * TV_STAGE + TV_SCORES + TV_META * 16 + (2 + 2) * 4 * TILE * 4 + 256;
 static_assert(TV_SMEM > CHAIN_TMEM_SMEM && TV_SMEM <= 232448, "no other CTA with tensor memory beside this one");
 static_assert(2 * TREE_PANEL_ROWS <= TILE, "the nodes' tile always comes in boxes");
 
+constexpr float TV_SMALL = 24.f;                               // bits of an fp32 sum
+static_assert(2 * TREE_DRAIN_16 * (TILE / JOINT_ROWS) < 65536, "lossy instructions of an accumulator, in sixteen bits");
 constexpr float TV_LOG2E = 1.44269504088896340736f;
 __device__ __forceinline__ uint64_t tv_pack(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ void tv_unpack(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
@@ -70,14 +72,15 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int req = blockIdx.x / a.n_splits, split = blockIdx.x - req * a.n_splits, c0 = blockIdx.y * TILE, range = blockIdx.z, panel0 = range * RANGE;
-  // shared memory: ring | scores [128 tokens][columns of a box] | descriptors | maxima [2][4 parts][128 rows] | barriers
+  // shared memory: ring | scores [128 tokens][columns of a box] | descriptors | maxima [2][4 parts][128 rows] | lossy instructions [2][4][128] | barriers
   const uint32_t sRing = smem_addr(smem_raw);
   const bool misaligned = (sRing & 1023u) != 0;                 // operand tiles need 1024-byte alignment for the swizzle
   const float* s_scores = reinterpret_cast<const float*>(smem_raw + TV_STAGES * TV_STAGE);
   const uint32_t sScores = sRing + TV_STAGES * TV_STAGE;
   int4* s_meta = reinterpret_cast<int4*>(smem_raw + TV_STAGES * TV_STAGE + TV_SCORES);
   float* s_max = reinterpret_cast<float*>(s_meta + TV_META);
-  unsigned char* tail = reinterpret_cast<unsigned char*>(s_max + 2 * 4 * TILE);
+  uint32_t* s_lossy = reinterpret_cast<uint32_t*>(s_max + 2 * 4 * TILE);
+  unsigned char* tail = reinterpret_cast<unsigned char*>(s_lossy + 2 * 4 * TILE);
   const uint32_t bars = smem_addr(tail);
   const uint32_t full = bars, empty = full + 8 * TV_STAGES, p_full = empty + 8 * TV_STAGES, p_done = p_full + 8, sc_full = p_done + 8, sc_empty = sc_full + 8;
   uint32_t* s_tmem_base = reinterpret_cast<uint32_t*>(tail + 8 * (2 * TV_STAGES + 4));
@@ -242,7 +245,27 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     float* const out = a.part_acc + (size_t)(r < 0 ? 0 : r) * v.d_kv + panel0 * PANEL;
     const int col0 = part * (COLS / 4);
     uint32_t stored = 0;
-    int since = 0, chain[RANGE / 2] = {};                         // tiles, and instructions, in the accumulators
+    int since = 0;                                                // tiles in the accumulators
+    // Instructions of this thread's tokens that cost the row's sums bits, sixteen bits per accumulator.  One costs nothing where the row's weights of its sixteen
+    // tokens fit one part (all of a size, or zeros: the products are short and their sums exact) or lie 2^TV_SMALL below the largest (shifted out of
+    // the sum instead of cutting it): a softmax that few tokens decide is summed without loss, and gets nothing back.
+    constexpr int LOSSY = (RANGE / 2 + 1) / 2;
+    uint32_t lossy[LOSSY] = {};
+    float give[RANGE / 2];                                        // what the accumulators get back
+    auto lost = [&]() {                                           // of all four parts, which have stored theirs
+      uint32_t n[LOSSY];
+#pragma unroll
+      for (int i = 0; i < LOSSY; ++i) {
+        const uint32_t* const p = s_lossy + i * 4 * TILE + row;
+        n[i] = p[0] + p[TILE] + p[2 * TILE] + p[3 * TILE];
+      }
+#pragma unroll
+      for (int e = 0; e < RANGE / 2; ++e) give[e] = 1.f + TREE_CUT_VALUES * (float)(n[e >> 1] >> 16 * (e & 1) & 0xffffu);
+    };
+    auto tell = [&]() {
+#pragma unroll
+      for (int i = 0; i < LOSSY; ++i) s_lossy[(4 * i + part) * TILE + row] = lossy[i];
+    };
     float kept = 1.f, largest = 0.f;                              // of the partial result, as it is stored
     auto read_out = [&](int c, float (&o)[32]) {                 // 32 of this thread's columns of the partial result
 #pragma unroll
@@ -258,7 +281,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         float fc = f;
 #pragma unroll
         for (int e = 0; e < RANGE / 2; ++e)
-          if (acc == (uint32_t)e) fc = f * (1.f + TREE_CUT_VALUES * (float)chain[e]);
+          if (acc == (uint32_t)e) fc = f * give[e];
         float d[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (fresh) {
           tmem_ld8(lanes + c + b, reinterpret_cast<uint32_t*>(d));
@@ -297,13 +320,15 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         __syncwarp();
         if (lane == 0) mbar_arrive(sc_empty);                     // the next tile's may come
         // the tile's maximum of the row, from the four threads that share it
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};      // two of each sixteen tokens
 #pragma unroll
-        for (int u = 0; u < 32; u += 4)
+        for (int u = 0; u < 16; u += 2)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], x[u + e]);
+          for (int e = 0; e < 4; ++e) mx[e] = fmaxf(mx[e], x[(e >> 1) * 16 + u + (e & 1)]);
+        const float mx0 = fmaxf(mx[0], mx[1]), mx1 = fmaxf(mx[2], mx[3]);
         float* const sm = s_max + (k & 1u) * 4 * TILE + row;
-        sm[part * TILE] = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        sm[part * TILE] = fmaxf(mx0, mx1);
+        if (since == a.drain) tell();
         // a wait that ran out in one warp ends the loop in the four of its quarter, here: none is left at a barrier
         if (!(ok = named_bar_and(1 + quarter, 128, ok && got))) break;
         const float most = fmaxf(fmaxf(sm[0], sm[TILE]), fmaxf(sm[2 * TILE], sm[3 * TILE])) * scale;
@@ -327,6 +352,11 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
           if constexpr (PARTS == 3) tree_split3(p, w[0][u >> 1], w[1][u >> 1], w[2][u >> 1]);
           else split_pair_16<BF16>(p, w[0][u >> 1], w[1][u >> 1]);
         }
+        uint32_t low[2] = {0u, 0u};                               // second parts of each sixteen weights: zero, or not
+#pragma unroll
+        for (int u = 0; u < 16; ++u) low[u >> 3] |= w[1][u];
+        const float small = top + (HEAD - TV_SMALL);
+        const uint32_t cuts = (low[0] != 0u && mx0 * scale > small ? 1u : 0u) + (low[1] != 0u && mx1 * scale > small ? 1u : 0u);
         if (k > 0) {
           const bool full_up = since == a.drain;
           float o[32];
@@ -334,6 +364,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
           ok = __all_sync(0xffffffffu, mbar_wait(p_done, (k - 1) & 1u, abort_flag));
           fence_after_sync();
           if (full_up && ok) {
+            lost();
             empty_onto(col0, o, f);
 #pragma unroll 1
             for (int c = col0 + 32; c < col0 + COLS / 4; c += 32) {
@@ -345,7 +376,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
             since = 0;
             kept = 1.f;
 #pragma unroll
-            for (int e = 0; e < RANGE / 2; ++e) chain[e] = 0;
+            for (int i = 0; i < LOSSY; ++i) lossy[i] = 0u;
           } else if (__any_sync(0xffffffffu, grow) && ok) {
             // seldom: this part's columns of the accumulators take the rows' factors
 #pragma unroll 1
@@ -363,9 +394,11 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         ++since;
         if (!ok) continue;
         const int reach = (min(m.y, panel0 + RANGE) - panel0 + 1) >> 1;
+        // two parts of sixteen tokens are two instructions (those of three bf16 parts: see TREE_CUT_VALUES); the small parts of an accumulator's first tile
+        // come before its sum has its size
 #pragma unroll
-        for (int e = 0; e < RANGE / 2; ++e)                       // (the small parts of an accumulator's first tile come before its sum has its size)
-          if (e < reach) chain[e] += vtile_boxes(m.z) * ((touched >> e) & 1u ? 2 : 1);
+        for (int e = 0; e < RANGE / 2; ++e)
+          if (e < reach) lossy[e >> 1] += cuts << (16 * (e & 1) + (int)((touched >> e) & 1u));
         touched |= (1u << reach) - 1u;
         if (any) {
 #pragma unroll
@@ -383,6 +416,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     float la, lb;
     tv_unpack(l_sum2, la, lb);
     s_max[part * TILE + row] = la + lb;                         // (behind the loop's last __syncthreads: nobody reads maxima any more)
+    tell();
     if (ok && k > 0) ok = __all_sync(0xffffffffu, mbar_wait(p_done, (k - 1) & 1u, abort_flag));
     fence_after_sync();
     named_bar_sync(1 + quarter, 128);
@@ -390,6 +424,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     // merge knows it from the split's widest class.
     largest = 0.f;
     if (ok && k > 0) {
+      lost();
 #pragma unroll 1
       for (int c = col0; c < col0 + COLS / 4; c += 32) {
         float o[32];

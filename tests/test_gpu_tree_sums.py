@@ -32,3 +32,42 @@ def test_components_behind_the_ranks_lose_nothing(B, dt, rank):  # noqa: F811
     _, bias = error_and_bias(out, want)
     assert abs(bias) <= 7e-7
     B.twkv_cache_destroy(h)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+def test_equal_weights_lose_nothing_in_the_sums_of_values(B, dt):  # noqa: F811
+    """Queries of zeros: all weights are one power of two, products are no longer than the values and their sums of 1250 tokens (2^11 of 2^11 steps, fp16) all but
+    exact.  What is left is the last product: 16 steps, at most three instructions each, in two sums: 24 x 2.15e-8 = 5.2e-7, and three roundings to nearest."""
+    b = Batch(402, [1250] * 40, [16] * 40, hq=16, hkv=2, dt=dt, ranks=200)
+    b.q = torch.zeros_like(b.q)
+    h = b.cache(B)
+    out, _ = run(B, h, b)
+    assert B.twkv_cache_status(h) == B.TWKV_OK
+    want, _ = b.want()
+    err, bias = error_and_bias(out, want)
+    assert abs(bias) <= 5.2e-7 and err <= 5.2e-7 + 3 * 2.0 ** -24
+    B.twkv_cache_destroy(h)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+def test_a_softmax_that_one_token_decides_loses_nothing(B, dt):  # noqa: F811
+    """One token of 1250 has a key, and every query lies along it: the others' weights are below e^-50.  Outputs are that token's value; its sixteen tokens
+    may count (twice 1.75e-8), and the last product as above."""
+    n, at = 40, 777
+    b = Batch(403, [1250] * n, [4] * n, hq=4, hkv=2, dt=dt, ranks=200)
+    b.nk = torch.zeros_like(b.nk)
+    keys = torch.zeros_like(b.xk)
+    for i in range(n):
+        keys[i * 1250 + at] = b.xk[i * 1250 + at]
+        k = b.rotate(b.rebuilt(keys[i * 1250 + at][None], torch.tensor([200]), b.uk), [at])[0]              # [KV heads, 128]
+        q = k * (60 / 128 ** -0.5 / (k * k).sum(-1, keepdim=True))                                          # scores of 60
+        for j in range(4):
+            b.q[b.offsets[i] + j] = q.repeat_interleave(2, 0).to(dt)
+    b.xk = keys
+    h = b.cache(B, shuffle=False)
+    out, _ = run(B, h, b)
+    assert B.twkv_cache_status(h) == B.TWKV_OK
+    want, _ = b.want()
+    err, bias = error_and_bias(out, want)
+    assert abs(bias) <= 5.6e-7 and err <= 5.6e-7 + 3 * 2.0 ** -24
+    B.twkv_cache_destroy(h)
