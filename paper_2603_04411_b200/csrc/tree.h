@@ -22,11 +22,12 @@ constexpr float TREE_CUT = 2.15e-8f;
 // Which of them count follows from the weights (tree_value.cu).  What it cannot see are values whose sums are exact (components that few tokens have): those
 // come out too large by what is given back, 1.75e-8 for an instruction, up to the drain below.
 constexpr float TREE_CUT_VALUES = 1.75e-8f;
-// Tiles that an accumulator of the value kernel takes before it is emptied, for fp32 outputs (of bf16 caches, whose three parts lengthen the chains) and
-// 16-bit ones: what the expectation leaves grows with the chain.  Error and time of fp32 outputs with 4 / 8 / 16 tiles: 8 x 4096 tokens bf16 7.6e-7 170 us /
-// 1.2e-6 153 us / 1.9e-6 140 us (plain fp32 sums 1.2e-6), 3 x 30745 bf16 8.1e-7 167 us / 1.4e-6 157 us (5.7e-7), 16 x 2048 fp16 9.3e-7 221 us /
-// 1.2e-6 199 us / 1.8e-6 187 us (1.2e-6).
-constexpr int TREE_DRAIN_F32 = 8, TREE_DRAIN_F32_BF16 = 4, TREE_DRAIN_16 = 128;
+// Boxes of sixteen tokens that an accumulator of the value kernel takes before it is emptied, for fp32 outputs (of bf16 caches, whose three parts lengthen the
+// chains) and 16-bit ones: what the expectation leaves grows with the chain.  (By boxes, since the tiles of mixed ranks hold one or two of them: eight
+// tiles of each took 313 us and 7.0e-7 for 48 x 100 tokens of any rank, 48 boxes 275 us and 7.3e-7.)  Error and time of fp32 outputs with 24 / 32 / 48:
+// 64 x 1024 tokens fp16 5.5e-7 147 us / 7.1e-7 147 us / 8.9e-7 143 us (plain fp32 sums 7.4e-7), bf16 6.2e-7 161 us / 8.6e-7 160 us / 1.1e-6 152 us (6.5e-7);
+// 16 x 2048 of any rank fp16 6.2e-7 198 us / 7.4e-7 192 us / 9.0e-7 181 us (1.1e-6), bf16 6.7e-7 237 us / 8.6e-7 227 us / 1.2e-6 211 us (9.4e-7).
+constexpr int TREE_DRAIN_F32 = 48, TREE_DRAIN_F32_BF16 = 24, TREE_DRAIN_16 = 1024;
 constexpr int TREE_MAX_RANGES = 4;               // ranges of panels whose sums a CTA of the value kernel keeps
 constexpr int TREE_MAX_SPLITS = 64;              // of a request's V tiles
 constexpr int TREE_PANEL_ROWS = 64;              // rows of a panel of the nodes' tiles
@@ -52,7 +53,7 @@ struct TreeCall {
   int q_box;            // rows of qop that a CTA takes at a time
   int m_cluster, m_rows, m_comps;     // CTAs of a cluster of the merge, query rows of a cluster, components that each CTA takes at a time
   int n_parts;          // parts that a weight, and a component of the merge, goes into products as
-  int drain;            // tiles that an accumulator of the value kernel takes before it is emptied
+  int drain;            // boxes of sixteen tokens that an accumulator of the value kernel takes before it is emptied
   int range;            // panels whose sums a CTA of the value kernel keeps
   int v_box;            // score columns that a CTA of the value kernel takes, at most 128
   // workspace

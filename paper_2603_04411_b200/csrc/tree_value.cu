@@ -38,7 +38,7 @@ static_assert(TV_SMEM > CHAIN_TMEM_SMEM && TV_SMEM <= 232448, "no other CTA with
 static_assert(2 * TREE_PANEL_ROWS <= TILE, "the nodes' tile always comes in boxes");
 
 constexpr float TV_SMALL = 24.f;                               // bits of an fp32 sum
-static_assert(2 * TREE_DRAIN_16 * (TILE / JOINT_ROWS) < 65536, "lossy instructions of an accumulator, in sixteen bits");
+static_assert(2 * (TREE_DRAIN_16 + TILE / JOINT_ROWS) < 65536, "lossy instructions of an accumulator, in sixteen bits");
 constexpr float TV_LOG2E = 1.44269504088896340736f;
 __device__ __forceinline__ uint64_t tv_pack(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
 __device__ __forceinline__ void tv_unpack(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
@@ -114,7 +114,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TV_REGS_LIGHT));
     uint32_t st = 0, st_ph = 0, n_loaded = 0;                   // ring stage and its phase; stages filled so far
-    int since = 0;                                              // tiles in the accumulators
+    int since = 0;                                              // boxes of tokens in the accumulators
     for (int k0 = 0; k0 < n_mine; k0 += TV_META) {
       if (warp == 0) {
         // the chunk's tiles that reach the range, in order
@@ -176,8 +176,8 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
             const int nb = vtile_boxes(m.z), end = min(m.y, panel0 + RANGE);
             if (!(ok = mbar_wait_thin(p_full, k & 1u, abort_flag))) break;
             fence_after_sync();
-            if (since == a.drain) { touched = 0; since = 0; }      // the weight warps have emptied the accumulators
-            ++since;
+            if (since >= a.drain) { touched = 0; since = 0; }      // the weight warps have emptied the accumulators
+            since += nb;
             for (int j = panel0; j < end; j += 2) {
               if (!(ok = mbar_wait_thin(full + 8 * st, st_ph, abort_flag))) break;
               fence_after_sync();
@@ -240,12 +240,12 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
     // Row of the partial results that this thread's column of the request stands for; -1: no node's.
     const int c = c0 + row, g = c / a.Rs, n = c - g * a.Rs, t = n / v.rep;
     const long long r = c < a.C && n < a.R && t < info.y ? ((long long)(req * a.T + t) * a.n_splits + split) * v.Hq + g * v.rep + n % v.rep : -1;
-    // The tensor core cuts its fp32 sums after every instruction, so an accumulator's error grows with the tiles in it.  After `drain` tiles it is emptied,
+    // The tensor core cuts its fp32 sums after every instruction, so an accumulator's error grows with the tiles in it.  After `drain` boxes of sixteen tokens it is emptied,
     // its expected loss given back, onto the partial result in memory: `stored`, accumulators that have been; worth `kept` of what it was then.
     float* const out = a.part_acc + (size_t)(r < 0 ? 0 : r) * v.d_kv + panel0 * PANEL;
     const int col0 = part * (COLS / 4);
     uint32_t stored = 0;
-    int since = 0;                                                // tiles in the accumulators
+    int since = 0;                                                // boxes of sixteen tokens in the accumulators
     // Instructions of this thread's tokens that cost the row's sums bits, sixteen bits per accumulator.  One costs nothing where the row's weights of its sixteen
     // tokens fit one part (all of a size, or zeros: the products are short and their sums exact) or lie 2^TV_SMALL below the largest (shifted out of
     // the sum instead of cutting it): a softmax that few tokens decide is summed without loss, and gets nothing back.
@@ -328,7 +328,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         const float mx0 = fmaxf(mx[0], mx[1]), mx1 = fmaxf(mx[2], mx[3]);
         float* const sm = s_max + (k & 1u) * 4 * TILE + row;
         sm[part * TILE] = fmaxf(mx0, mx1);
-        if (since == a.drain) tell();
+        if (since >= a.drain) tell();
         // a wait that ran out in one warp ends the loop in the four of its quarter, here: none is left at a barrier
         if (!(ok = named_bar_and(1 + quarter, 128, ok && got))) break;
         const float most = fmaxf(fmaxf(sm[0], sm[TILE]), fmaxf(sm[2 * TILE], sm[3 * TILE])) * scale;
@@ -358,7 +358,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
         const float small = top + (HEAD - TV_SMALL);
         const uint32_t cuts = (low[0] != 0u && mx0 * scale > small ? 1u : 0u) + (low[1] != 0u && mx1 * scale > small ? 1u : 0u);
         if (k > 0) {
-          const bool full_up = since == a.drain;
+          const bool full_up = since >= a.drain;
           float o[32];
           if (full_up) read_out(col0, o);
           ok = __all_sync(0xffffffffu, mbar_wait(p_done, (k - 1) & 1u, abort_flag));
@@ -391,7 +391,7 @@ tree_value_kernel(const __grid_constant__ CUtensorMap map_blocks, const __grid_c
             }
           }
         }
-        ++since;
+        since += vtile_boxes(m.z);
         if (!ok) continue;
         const int reach = (min(m.y, panel0 + RANGE) - panel0 + 1) >> 1;
         // two parts of sixteen tokens are two instructions (those of three bf16 parts: see TREE_CUT_VALUES); the small parts of an accumulator's first tile

@@ -71,3 +71,23 @@ def test_a_softmax_that_one_token_decides_loses_nothing(B, dt):  # noqa: F811
     err, bias = error_and_bias(out, want)
     assert abs(bias) <= 5.6e-7 and err <= 5.6e-7 + 3 * 2.0 ** -24
     B.twkv_cache_destroy(h)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("ctx,nodes,hq,hkv,rank", [
+    ([700] * 37, [13] * 37, 16, 4, "any"),
+    ([1024] * 24, [8] * 24, 32, 8, 256),                      # full tiles, so that accumulators are emptied on the way
+    ([4096] * 2, [5] * 2, 4, 2, 256),
+    ([20000], [4], 4, 2, "any"),
+])
+def test_errors_are_those_of_fp32_sums(B, dt, ctx, nodes, hq, hkv, rank):  # noqa: F811
+    """Relative error of the whole output, with the bound of test_fp32_outputs_are_as_good_as_fp32_sums: fp32 sums of n terms, each step rounded, wander by
+    sqrt(n) 2^-24 / sqrt(3).  Twice what keys (d products, doubled by queries, scores and weights) and values (all tokens) come to."""
+    b = Batch(404, ctx, nodes, hq=hq, hkv=hkv, dt=dt, ranks=rank)
+    h = b.cache(B)
+    out, _ = run(B, h, b)
+    assert B.twkv_cache_status(h) == B.TWKV_OK
+    want, _ = b.want()
+    err, _ = error_and_bias(out, want)
+    assert err <= 2 * (2 * b.d ** 0.5 + (max(ctx) + max(nodes)) ** 0.5) * 2.0 ** -24 / 3 ** 0.5
+    B.twkv_cache_destroy(h)
