@@ -148,6 +148,23 @@ def _stream(stream=None):
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+# The tree operators' ids, counts and tokens are int32: wider ones (argmax gives int64) would be read as pairs, without an error.  The calls compare the
+# types in one chain, 0.05 us an array; which of them is wrong is found out afterwards.
+_I32 = torch.int32
+
+
+def _not_int32(where, **arrays):
+    for name, t in arrays.items():
+        if t.dtype is not _I32:
+            raise TypeError(f"{where}: {name} must be int32, not {t.dtype}")
+
+
+def _width(where, size, **arrays):
+    for name, t in arrays.items():
+        if t.element_size() != size or (size == 8 and t.is_floating_point()):
+            raise TypeError(f"{where}: {name} must have elements of {size} bytes, not {t.dtype}")
+
+
 def dtype_code(dt) -> int:
     return {torch.float16: TWKV_F16, torch.bfloat16: TWKV_BF16, torch.float32: TWKV_F32}[dt]
 
@@ -254,6 +271,11 @@ def twkv_gate_soft(cache, layer, K, V, m_k=None, m_v=None, xh_k=None, xh_v=None,
 def twkv_slot_map(cache, layer, req_seqs, req_lens, offsets, seq_ids, positions, starts=None, stream=None):
     """Request lengths -> offsets [n_req + 1], seq_ids and positions of every new row (int32 CUDA tensors; the two last have room for
     the rows the caller expects at most).  starts=None: every request starts behind the tokens cached for its sequence in `layer`."""
+    if not (req_seqs.dtype is req_lens.dtype is offsets.dtype is seq_ids.dtype is positions.dtype is _I32):
+        _not_int32("twkv_slot_map", req_seqs=req_seqs, req_lens=req_lens, offsets=offsets, seq_ids=seq_ids, positions=positions)
+    if starts is not None:
+        _not_int32("twkv_slot_map", starts=starts)
+        assert starts.numel() == req_seqs.numel()
     assert req_lens.numel() == req_seqs.numel() and offsets.numel() == req_seqs.numel() + 1 and seq_ids.numel() == positions.numel()
     _check(lib.twkv_slot_map(cache, layer, _ptr(req_seqs), _ptr(req_lens), _ptr(starts), req_seqs.numel(), seq_ids.numel(), _ptr(offsets),
                              _ptr(seq_ids), _ptr(positions), _stream(stream)), "twkv_slot_map")
@@ -261,7 +283,11 @@ def twkv_slot_map(cache, layer, req_seqs, req_lens, offsets, seq_ids, positions,
 
 def twkv_tree_map(cache, offsets, parents, positions, masks, max_nodes=TREE_MAX_NODES, stream=None):
     """Parents -> positions (int32, in place: every tree's first row is given) and ancestor masks (int64 CUDA tensor, one bit per node)."""
-    assert positions.numel() == parents.numel() and masks.numel() == parents.numel() and masks.element_size() == 8
+    if not (offsets.dtype is parents.dtype is positions.dtype is _I32):
+        _not_int32("twkv_tree_map", offsets=offsets, parents=parents, positions=positions)
+    if masks.element_size() != 8:
+        _width("twkv_tree_map", 8, masks=masks)
+    assert positions.numel() == parents.numel() and masks.numel() == parents.numel()
     _check(lib.twkv_tree_map(cache, _ptr(offsets), _ptr(parents), offsets.numel() - 1, parents.numel(), max_nodes, _ptr(positions), _ptr(masks),
                              _stream(stream)), "twkv_tree_map")
 
@@ -275,8 +301,12 @@ def twkv_tree_attn(cache, layer, q, K, V, levels, req_seqs, offsets, positions, 
     K / V: [n_rows, d_kv] spectral states of the nodes, levels: [n_rows, 2] their ranks; workspace: 1-D uint8 CUDA tensor of
     twkv_tree_required_bytes(cache, n_req, max_nodes) bytes (fewer: several passes)."""
     n = q.shape[0]
+    if not (req_seqs.dtype is offsets.dtype is positions.dtype is _I32):
+        _not_int32("twkv_tree_attn", req_seqs=req_seqs, offsets=offsets, positions=positions)
+    _width("twkv_tree_attn", 2, q=q, K=K, V=V, levels=levels)
+    _width("twkv_tree_attn", 8, masks=masks)
     assert K.shape[0] == n and V.shape[0] == n and levels.numel() == 2 * n and positions.numel() == n and masks.numel() == n and out.shape[0] == n
-    assert offsets.numel() == req_seqs.numel() + 1 and masks.element_size() == 8 and levels.element_size() == 2
+    assert offsets.numel() == req_seqs.numel() + 1
     _check(lib.twkv_tree_attn(cache, layer, _ptr(q), _ptr(K), _ptr(V), _ptr(levels), _ptr(req_seqs), _ptr(offsets), _ptr(positions), _ptr(masks),
                               req_seqs.numel(), n, max_nodes, _ptr(out), _ptr(workspace), workspace.numel() * workspace.element_size(),
                               _stream(stream)), "twkv_tree_attn")
@@ -284,6 +314,8 @@ def twkv_tree_attn(cache, layer, q, K, V, levels, req_seqs, offsets, positions, 
 
 def twkv_tree_accept(cache, offsets, parents, draft, target, n_accepted, rows, next_tokens, max_nodes=TREE_MAX_NODES, stream=None):
     """Drafted and chosen tokens -> kept nodes per request, their rows one request behind the other, and every request's next token."""
+    if not (offsets.dtype is parents.dtype is draft.dtype is target.dtype is n_accepted.dtype is rows.dtype is next_tokens.dtype is _I32):
+        _not_int32("twkv_tree_accept", offsets=offsets, parents=parents, draft=draft, target=target, n_accepted=n_accepted, rows=rows, next_tokens=next_tokens)
     n, n_req = parents.numel(), offsets.numel() - 1
     assert draft.numel() == n and target.numel() == n and rows.numel() == n and n_accepted.numel() == n_req and next_tokens.numel() == n_req
     _check(lib.twkv_tree_accept(cache, _ptr(offsets), _ptr(parents), _ptr(draft), _ptr(target), n_req, n, max_nodes, _ptr(n_accepted), _ptr(rows),
