@@ -254,7 +254,10 @@ twkv_status twkv_tree_map(twkv_cache* cache, const int32_t* offsets, const int32
  *              for one request, is taken as well: the requests then run in several passes.  It holds nothing between calls, and calls that
  *              overlap on the GPU must not share it (nor the cache's scratch).
  * A request with an id, offset, rank or position out of range, or whose sequence or rows an earlier one names, gets zeros (where its rows
- * are its own) and the sticky status is set.  A node whose V state is not finite makes the outputs of the nodes that see it NaN, no others.
+ * are its own) and the sticky status is set.  A node whose K or V state (within its rank) is not finite makes the outputs of the nodes that
+ * see it NaN, no others.
+ * Keys and queries enter the score product as f16: a bf16 query beyond 65504 is clamped and sets TWKV_ERR_DEVICE_CHECK, one below 2^-14 keeps 2^-25 absolute;
+ * rotated keys are carried to 2^-21 of their size and must stay within 65504 (TWKV_DEBUG=1 at cache creation reports one that does not).  As in a decode call.
  */
 size_t twkv_tree_required_bytes(const twkv_cache* cache, int n_req, int max_nodes);
 twkv_status twkv_tree_attn(twkv_cache* cache, int layer, const void* q, const void* K, const void* V, const uint16_t* levels,
