@@ -28,7 +28,8 @@ struct DevView {
   int L, Hq, Hkv, rep, d_kv, NC, S, tmax, NT, TPS, n_blocks, dtype, out_dtype, NK, max_partials;
   float tau, sm_scale;
   int debug;                 // TWKV_DEBUG=1 at cache creation: extra device-side checks (rotated keys inside the f16 range)
-  int* status;               // [8]: [0] sticky status, [1] next free block, [2] rows listed for the gate fix-up, [3] its finished CTAs
+  int* status;               // [8]: [0] sticky status, [1] next free block, [2] rows listed for the gate fix-up, [3] its finished CTAs, [4] finished CTAs of the
+                             //      walk over drafted trees (zero between calls, as [3])
   int* pflags;               // [batch][2]: piece accepted, piece holds an invalid token (scratch of one compress call)
   int batch;                 // pieces of a compress call whose bookkeeping is launched together
   // RoPE tables, one float4 per pair of frequencies (2t, 2t + 1): (cos_2t, cos_2t+1, sin_2t, sin_2t+1)
@@ -67,7 +68,7 @@ struct DevView {
   int* evict_map;            // [2][NT * 128]  new global slot of every K / V slot of the sequence, -1 = dropped
   int* evict_fill;           // [2][NC]  survivors per key
   int* wave_buf;             // [3 * TWKV_PREFILL_MAX_QUERIES]  the host's tables of a prefill call; in waves: sequence, row and position of
-                             // the queries, wave by wave
+                             // the queries, wave by wave; while drafted trees are walked, a 64-bit path per request
   int4* klist;               // [NT]  K tiles of the current decode call, widest class first: (tile, class | n_valid << 8, base block, query slot);
                              //       a joint tile: (~ its number, class | 128 << 8, 0, query slot)
   int4* kpairs;              // [NT + 64]  the same list as items of two tiles of one class (entries 2 i, 2 i + 1) for the CTA-pair kernel;
