@@ -273,12 +273,14 @@ def twkv_slot_map(cache, layer, req_seqs, req_lens, offsets, seq_ids, positions,
     the rows the caller expects at most).  starts=None: every request starts behind the tokens cached for its sequence in `layer`."""
     if not (req_seqs.dtype is req_lens.dtype is offsets.dtype is seq_ids.dtype is positions.dtype is _I32):
         _not_int32("twkv_slot_map", req_seqs=req_seqs, req_lens=req_lens, offsets=offsets, seq_ids=seq_ids, positions=positions)
+    n, rows = req_seqs.numel(), seq_ids.numel()
     if starts is not None:
-        _not_int32("twkv_slot_map", starts=starts)
-        assert starts.numel() == req_seqs.numel()
-    assert req_lens.numel() == req_seqs.numel() and offsets.numel() == req_seqs.numel() + 1 and seq_ids.numel() == positions.numel()
-    _check(lib.twkv_slot_map(cache, layer, _ptr(req_seqs), _ptr(req_lens), _ptr(starts), req_seqs.numel(), seq_ids.numel(), _ptr(offsets),
-                             _ptr(seq_ids), _ptr(positions), _stream(stream)), "twkv_slot_map")
+        if starts.dtype is not _I32:
+            _not_int32("twkv_slot_map", starts=starts)
+        assert starts.numel() == n
+    assert req_lens.numel() == n and offsets.numel() == n + 1 and positions.numel() == rows
+    _check(lib.twkv_slot_map(cache, layer, _ptr(req_seqs), _ptr(req_lens), _ptr(starts), n, rows, _ptr(offsets), _ptr(seq_ids), _ptr(positions),
+                             _stream(stream)), "twkv_slot_map")
 
 
 def twkv_tree_map(cache, offsets, parents, positions, masks, max_nodes=TREE_MAX_NODES, stream=None):
@@ -287,8 +289,9 @@ def twkv_tree_map(cache, offsets, parents, positions, masks, max_nodes=TREE_MAX_
         _not_int32("twkv_tree_map", offsets=offsets, parents=parents, positions=positions)
     if masks.element_size() != 8:
         _width("twkv_tree_map", 8, masks=masks)
-    assert positions.numel() == parents.numel() and masks.numel() == parents.numel()
-    _check(lib.twkv_tree_map(cache, _ptr(offsets), _ptr(parents), offsets.numel() - 1, parents.numel(), max_nodes, _ptr(positions), _ptr(masks),
+    n = parents.numel()
+    assert positions.numel() == n and masks.numel() == n
+    _check(lib.twkv_tree_map(cache, _ptr(offsets), _ptr(parents), offsets.numel() - 1, n, max_nodes, _ptr(positions), _ptr(masks),
                              _stream(stream)), "twkv_tree_map")
 
 
