@@ -80,13 +80,14 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
       float4 y[4];
       float l[4];
       float4 x[4];
+      int cls[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const int sp = s0 + k * lanes;
         if constexpr (!BF16) x[k] = sp < used ? a.part_x[row + (size_t)sp * v.Hq] : make_float4(0.f, 0.f, 0.f, 0.f);
         y[k] = sp < used ? a.part_m[row + (size_t)sp * v.Hq] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
         l[k] = sp < used ? a.part_l[row + (size_t)sp * v.Hq] : 0.f;
-        if (exacting && sp < used) wide = max(wide, a.part_cls[req * a.n_splits + sp]);
+        cls[k] = sp < used ? a.part_cls[req * a.n_splits + sp] : 0;
       }
       const float m = fmaxf(fmaxf(fmaxf(y[0].x, y[1].x), fmaxf(y[2].x, y[3].x)), most);
       sum *= most == -INFINITY ? 0.f : tm_ex2(most - m);        // (one that is not a number stays one)
@@ -95,6 +96,7 @@ __global__ void __launch_bounds__(TM_THREADS, 2) tree_merge_kernel(const __grid_
       for (int k = 0; k < 4; ++k) {
         const float w = y[k].x == -INFINITY ? 0.f : tm_ex2(y[k].x - m);
         sum += l[k] * w;
+        wide = max(wide, cls[k]);
         if constexpr (!BF16) {                                   // a range's components are relative to its own reference
           const float ref[TREE_MAX_RANGES] = {y[k].x, y[k].y, y[k].z, y[k].w}, big[TREE_MAX_RANGES] = {x[k].x, x[k].y, x[k].z, x[k].w};
           float of_split = 0.f;
