@@ -13,8 +13,8 @@
 // latency bound the kernel: 5600 cycles per narrow tile).  What a row's weights are relative to, top[c], is its largest score so far (fp16: 2^-7 of it,
 // so that what is 2^31 below the maximum is still more than zero), moved only when that has grown by more than 2^8 (f16 holds 2^15): the accumulators
 // are rescaled seldom, by the warps that own their lanes.  The merge brings the splits' parts together.
-// A tile of four panels takes 2.4 to 2.7 us (16 sequences of 32768 tokens, 128 CTAs), of which the products are 1.1: 8700 warp instructions form its
-// 16384 weights, 46 % of the issue slots of that time.
+// A tile of four panels takes 2.4 to 2.7 us (16 sequences of 32768 tokens, 128 CTAs), of which the products are 1.1: 8900 warp instructions form its
+// 16384 weights, 48 % of the issue slots of that time.
 // Tiles that are at most half full, and the nodes' tile, are read by the boxes of sixteen rows that hold tokens.
 //
 // Warp roles (640 threads, one CTA per SM): 0 TMA producer of V panels, 1 MMA issuer (owns the TMEM allocation), 2 TMA producer of scores, 4-19 weights
